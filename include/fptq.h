@@ -234,6 +234,69 @@ int fptq_w4a4_linear_scratch(const void *xq_packed, const void *w_packed, int64_
 int fptq_w4a4_linear_ref(const void *xq_packed, const void *w_packed, int64_t M, int64_t N, int64_t K, float s_a,
                          const float *s_w, const float *row_out_scale, void *y_bf16, int32_t *acc_dbg, void *stream);
 
+/*
+ * What a decoder layer does between its QKV and its O projection: rotate queries and keys by position, keep keys and values in a paged
+ * 8-bit cache, and attend, over whole prompts or over the cache.  The calls work on `tokens` new tokens of `sequences` sequences, packed
+ * one sequence after the other.
+ *   tokens                      up to 2^24; 0: nothing is done
+ *   heads, kv_heads, head_dim   query heads, a multiple of kv_heads; head h reads key and value head h / (heads / kv_heads); head_dim 64 or 128
+ *   fptq_heads                  bf16 rows: value d of head h of token t is data[t * token_stride + h * head_stride + d].  Strides are in
+ *                               values, multiples of 8 from 0 to 2^24 - 8; data is 16-byte aligned.  So parts of the QKV projection's rows serve as they are.
+ *   cu                          device, int32 [sequences + 1]: sequence b's tokens are cu[b] .. cu[b + 1] - 1 (none is allowed); NULL: one token
+ *                               each, tokens == sequences.  Rows of no sequence are not written.
+ *   lengths                     device, int32 [sequences]: a sequence's tokens in the cache, the new ones included; its last new token is at position lengths[b] - 1
+ *   table, table_width          device, int32 [sequences x table_width]: pages of a sequence in order, 64 tokens each
+ * Array contents that cannot be checked before the launch are checked on the device: a page number outside the cache, or a position that
+ * the table does not reach, is no page (nothing is written there and nothing there is seen); a position outside the rotation's table makes NaN.
+ */
+typedef struct {
+    const void *data;
+    int64_t token_stride, head_stride;
+} fptq_heads;
+
+/*
+ * The cache: `pages` pages of 64 tokens of one sequence each.  Of every page and kv head the codes (e4m3, 64 * head_dim bytes) and one fp32 scale, a
+ * power of two between 2^-100 and 2^120: value = code * scale.  16-byte aligned, [pages x kv_heads x 64 * head_dim] and [pages x kv_heads].
+ *   keys    of a page and head lie as [head_dim / 64][64 tokens][64 values]
+ *   values  as [4][head_dim][16 tokens]
+ * No initialisation is needed: what lies past a sequence's length is never used.
+ */
+typedef struct {
+    void *key_codes, *value_codes;
+    float *key_scales, *value_scales;
+    int64_t pages;
+} fptq_cache;
+
+/*
+ * Rotates q and k by position and appends k and v to the cache.
+ *   rope       device, fp32 [positions x 2 x rope_dims / 2], 16-byte aligned: cosines, then sines, of every position's angles.  The first rope_dims values
+ *              of a head are rotated, a multiple of 16 up to head_dim; 0 and NULL: none.  (y1, y2) = (x1 c - x2 s, x2 c + x1 s), in fp32.
+ *   interleaved  pair i is values 2 i and 2 i + 1, else i and i + rope_dims / 2
+ *   q_out      bf16 [tokens x heads x head_dim] contiguous: rotated queries
+ *   k_out      the same of the keys, [tokens x kv_heads x head_dim], or NULL
+ * Codes are rounded once, from the fp32 keys.  A page's scale is the smallest power of two s with max |x| <= 448 s over its tokens (2^-100 at least); new
+ * tokens that begin in the middle of a page keep the scale it has or raise it, and then its older codes are rounded again.  Values that are not finite
+ * do not count for the scale and are stored as NaN.  No page may belong to two sequences that are appended to.
+ */
+int fptq_cache_append(const fptq_heads *q, const fptq_heads *k, const fptq_heads *v, int64_t tokens, int64_t sequences, int heads, int kv_heads,
+                      int head_dim, const float *rope, int64_t positions, int rope_dims, int interleaved, const fptq_cache *cache, const int32_t *table,
+                      int64_t table_width, const int32_t *lengths, const int32_t *cu, void *q_out, void *k_out, void *stream);
+
+/*
+ * out = softmax(scale * q k^T) v over the cache, bf16 [tokens x heads x head_dim] contiguous.  A token sees its sequence up to itself; one at a
+ * negative position sees nothing and gets zeros.
+ *   scratch    device, 256-byte aligned, at least fptq_cached_attention_scratch_bytes(...) bytes (which may be 0), or NULL.  With it, long sequences are
+ *              shared out to many compute units.  Its contents need no initialisation and mean nothing afterwards.  Calls that share it must not overlap in time.
+ */
+int64_t fptq_cached_attention_scratch_bytes(int64_t tokens, int64_t sequences, int heads, int kv_heads, int head_dim, int64_t table_width);
+int fptq_cached_attention(const fptq_heads *q, int64_t tokens, int64_t sequences, int heads, int kv_heads, int head_dim, float scale,
+                          const fptq_cache *cache, const int32_t *table, int64_t table_width, const int32_t *lengths, const int32_t *cu, void *out,
+                          void *scratch, int64_t scratch_bytes, void *stream);
+
+/* out = softmax(scale * q k^T) v of every token over its prompt up to itself, bf16 [tokens x heads x head_dim] contiguous; cu is required. */
+int fptq_prompt_attention(const fptq_heads *q, const fptq_heads *k, const fptq_heads *v, int64_t tokens, int64_t sequences, int heads, int kv_heads,
+                          int head_dim, float scale, const int32_t *cu, void *out, void *stream);
+
 /* Library layout -> one int8 per value, [rows x K] row-major (for parity checks and debugging). */
 int fptq_unpack(const void *packed, int64_t rows, int64_t K, int8_t *out_int8, void *stream);
 

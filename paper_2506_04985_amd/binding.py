@@ -21,12 +21,22 @@ EXPORTS = ["fptq_version", "fptq_last_error", "fptq_init", "fptq_packed_bytes", 
            "fptq_quantize_act_hadamard", "fptq_quantize_act_dynamic", "fptq_quantize_act_asym",
            "fptq_weight_row_sums", "fptq_w4a4_linear_zp", "fptq_residual_norm_quantize",
            "fptq_w4a4_linear", "fptq_w4a4_linear_ref", "fptq_unpack", "fptq_linear_workspace_bytes", "fptq_w4a4_linear_ws",
-           "fptq_w4a4_linear_noalloc", "fptq_linear_scratch_bytes", "fptq_w4a4_linear_scratch"]
+           "fptq_w4a4_linear_noalloc", "fptq_linear_scratch_bytes", "fptq_w4a4_linear_scratch",
+           "fptq_cache_append", "fptq_cached_attention_scratch_bytes", "fptq_cached_attention", "fptq_prompt_attention"]
 TESTING_EXPORTS = ["fptq_set_gemm_tile", "fptq_set_gemm_map", "fptq_set_decode_shape", "fptq_set_linear_prefill",
                    "fptq_linear_launch_plan"]
 
 _lib = None
 _native = None      # the native fast path (csrc/fptq_native.cpp), loaded with the library: a call returns None where it leaves the call to Python
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("key_codes", ctypes.c_void_p), ("value_codes", ctypes.c_void_p), ("key_scales", ctypes.c_void_p), ("value_scales", ctypes.c_void_p),
+                ("pages", ctypes.c_int64)]
 
 
 class FptqError(RuntimeError):
@@ -88,6 +98,15 @@ def lib():
         L.fptq_linear_scratch_bytes.argtypes = [i64, i64, i64]
         L.fptq_w4a4_linear_scratch.restype = i32
         L.fptq_w4a4_linear_scratch.argtypes = [p, p, i64, i64, i64, f32, p, p, i32, p, p, p, p, i64, p]
+        H, C = ctypes.POINTER(_Heads), ctypes.POINTER(_Cache)
+        L.fptq_cache_append.restype = i32
+        L.fptq_cache_append.argtypes = [H, H, H, i64, i64, i32, i32, i32, p, i64, i32, i32, C, p, i64, p, p, p, p, p]
+        L.fptq_cached_attention_scratch_bytes.restype = i64
+        L.fptq_cached_attention_scratch_bytes.argtypes = [i64, i64, i32, i32, i32, i64]
+        L.fptq_cached_attention.restype = i32
+        L.fptq_cached_attention.argtypes = [H, i64, i64, i32, i32, i32, f32, C, p, i64, p, p, p, p, i64, p]
+        L.fptq_prompt_attention.restype = i32
+        L.fptq_prompt_attention.argtypes = [H, H, H, i64, i64, i32, i32, i32, f32, p, p, p]
         try:
             from . import _native as native      # built next to this file, with the library
         except ImportError as e:                 # only the library was built, or for another torch: the Python path makes the same calls
@@ -369,6 +388,141 @@ def fptq_w4a4_linear_noalloc(xq, wq, M, N, K, s_a, s_w, row_out_scale=None, out=
 
 def fptq_w4a4_linear_ref(xq, wq, M, N, K, s_a, s_w, row_out_scale=None, out=None, want_acc=False, acc=None):
     return _linear(lib().fptq_w4a4_linear_ref, xq, wq, M, N, K, s_a, s_w, row_out_scale, out, want_acc, acc)
+
+
+class Cache:
+    """A paged 8-bit cache of keys and values: `pages` pages of 64 tokens of one sequence.  key_codes and value_codes are uint8
+    [pages, kv_heads, 64 * head_dim], key_scales and value_scales fp32 [pages, kv_heads] (the layout: include/fptq.h)."""
+
+    __slots__ = ("key_codes", "value_codes", "key_scales", "value_scales")
+
+    def __init__(self, key_codes, value_codes, key_scales, value_scales):
+        for t, dtype, name in ((key_codes, torch.uint8, "key_codes"), (value_codes, torch.uint8, "value_codes"),
+                               (key_scales, torch.float32, "key_scales"), (value_scales, torch.float32, "value_scales")):
+            _dev(t, dtype, name)
+        if key_codes.dim() != 3 or value_codes.shape != key_codes.shape or key_codes.shape[2] % 64 or not (key_scales.shape == value_scales.shape == key_codes.shape[:2]):
+            raise FptqError(-2, "a cache has codes [pages, kv_heads, 64 * head_dim] and scales [pages, kv_heads]")
+        self.key_codes, self.value_codes, self.key_scales, self.value_scales = key_codes, value_codes, key_scales, value_scales
+
+    @classmethod
+    def empty(cls, pages, kv_heads, head_dim, device="cuda"):
+        """Room for pages * 64 tokens; needs no initialisation."""
+        codes = [torch.empty((pages, kv_heads, 64 * head_dim), dtype=torch.uint8, device=device) for _ in range(2)]
+        return cls(*codes, *(torch.empty((pages, kv_heads), dtype=torch.float32, device=device) for _ in range(2)))
+
+
+def _heads(t, name, like=None):
+    """bf16 [tokens, heads, head_dim] device tensor, any strides but the last."""
+    if not (t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3 and t.stride(2) == 1):
+        raise TypeError(f"{name}: need a bf16 device tensor [tokens, heads, head_dim] whose last dimension is contiguous")
+    if like is not None and (t.shape[0] != like.shape[0] or t.shape[2] != like.shape[2]):
+        raise FptqError(-2, f"{name}: {tuple(t.shape)} does not go with q's {tuple(like.shape)}")
+    return _Heads(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+
+
+def _sequences(cache, table, lengths, cu, kv_heads, D):
+    _dev(table, torch.int32, "table")
+    _dev(lengths, torch.int32, "lengths")
+    sequences = lengths.numel()
+    if table.dim() != 2 or table.shape[0] != sequences:
+        raise FptqError(-2, f"table: {tuple(table.shape)} does not go with {sequences} lengths")
+    if tuple(cache.key_codes.shape[1:]) != (kv_heads, 64 * D):
+        raise FptqError(-2, f"the cache's pages hold {tuple(cache.key_codes.shape[1:])} bytes, heads of {kv_heads} x {D} need {(kv_heads, 64 * D)}")
+    _cu(cu, sequences)
+    handle = _Cache(cache.key_codes.data_ptr(), cache.value_codes.data_ptr(), cache.key_scales.data_ptr(), cache.value_scales.data_ptr(), cache.key_codes.shape[0])
+    return sequences, handle
+
+
+def _cu(cu, sequences):
+    if cu is not None:
+        _dev(cu, torch.int32, "cu")
+        if cu.numel() != sequences + 1:
+            raise FptqError(-2, f"cu: {cu.numel()} entries, {sequences} sequences need {sequences + 1}")
+
+
+def _rows(out, T, H, D, like, name):
+    if out is None:
+        return torch.empty((T, H, D), dtype=torch.bfloat16, device=like.device)
+    _dev(out, torch.bfloat16, name)
+    if out.numel() < T * H * D:
+        raise FptqError(-3, f"{name}: {out.numel()} values, need {T * H * D}")
+    return out
+
+
+def fptq_cache_append(q, k, v, rope, cache, table, lengths, cu=None, interleaved=False, want_k=False, q_out=None, k_out=None):
+    """Rotates q [T, heads, D] and k [T, kv_heads, D] (bf16, strided rows) by position and appends k and v to the cache.  rope: fp32
+    [positions, 2, R / 2] cosines and sines, or None.  lengths int32 [B] count the new tokens; cu int32 [B + 1], or None for one
+    token a sequence.  Returns (rotated q, rotated k or None), bf16 contiguous."""
+    done = None if _native is None else _native.cache_append(q, k, v, rope, cache.key_codes, cache.value_codes, cache.key_scales, cache.value_scales,
+                                                             table, lengths, cu, interleaved, want_k, q_out, k_out)
+    if done is not None:
+        return done
+    hq = _heads(q, "q")
+    hk, hv = _heads(k, "k", q), _heads(v, "v", q)
+    (T, H, D), J = q.shape, k.shape[1]
+    if v.shape[1] != J:
+        raise FptqError(-2, f"k has {J} heads, v {v.shape[1]}")
+    B, handle = _sequences(cache, table, lengths, cu, J, D)
+    positions = rope_dims = 0
+    if rope is not None:
+        _dev(rope, torch.float32, "rope")
+        if rope.dim() != 3 or rope.shape[1] != 2:
+            raise FptqError(-2, f"rope: {tuple(rope.shape)}, need [positions, 2, rope_dims / 2]")
+        positions, rope_dims = rope.shape[0], 2 * rope.shape[2]
+    q_out = _rows(q_out, T, H, D, q, "q_out")
+    if k_out is not None or want_k:
+        k_out = _rows(k_out, T, J, D, q, "k_out")
+    _check(lib().fptq_cache_append(hq, hk, hv, T, B, H, J, D, _ptr(rope), positions, rope_dims, int(interleaved), handle, _ptr(table), table.shape[1],
+                                   _ptr(lengths), _ptr(cu), _ptr(q_out), _ptr(k_out), _stream()))
+    return q_out, k_out
+
+
+def fptq_cached_attention_scratch_bytes(tokens, sequences, heads, kv_heads, head_dim, table_width):
+    """Bytes of scratch fptq_cached_attention would use (0: it would not use any)."""
+    n = lib().fptq_cached_attention_scratch_bytes(tokens, sequences, heads, kv_heads, head_dim, table_width)
+    if n < 0:
+        _check(int(n))
+    return int(n)
+
+
+def fptq_cached_attention(q, cache, table, lengths, cu=None, scale=None, out=None, scratch=None):
+    """Attention of each sequence's last tokens, q bf16 [T, heads, D] (strided rows), over its cache: bf16 [T, heads, D].  scale: 1 / sqrt(D) if
+    None.  Scratch comes from torch's allocator unless given: a capture not made through torch, which would have no pool of its own, has to give it."""
+    done = None if _native is None else _native.cached_attention(q, cache.key_codes, cache.value_codes, cache.key_scales, cache.value_scales, table, lengths,
+                                                                 cu, scale, out, scratch)
+    if done is not None:
+        return done
+    hq = _heads(q, "q")
+    T, H, D = q.shape
+    J = cache.key_codes.shape[1]
+    B, handle = _sequences(cache, table, lengths, cu, J, D)
+    out = _rows(out, T, H, D, q, "out")
+    if scratch is None:
+        n = lib().fptq_cached_attention_scratch_bytes(T, B, H, J, D, table.shape[1])
+        # as in _scratch: only the order of its own stream guards it once the call has returned
+        if n > 0 and q.device.index == torch.cuda.current_device():
+            scratch = torch.empty(n, dtype=torch.uint8, device=q.device)
+    else:
+        _dev(scratch, torch.uint8, "scratch")
+    _check(lib().fptq_cached_attention(hq, T, B, H, J, D, D ** -0.5 if scale is None else float(scale), handle, _ptr(table), table.shape[1], _ptr(lengths),
+                                       _ptr(cu), _ptr(out), _ptr(scratch), 0 if scratch is None else scratch.numel(), _stream()))
+    return out
+
+
+def fptq_prompt_attention(q, k, v, cu, scale=None, out=None):
+    """Causal attention within packed prompts: q bf16 [T, heads, D], k, v [T, kv_heads, D] (strided rows), cu int32 [B + 1]: bf16 [T, heads, D]."""
+    done = None if _native is None else _native.prompt_attention(q, k, v, cu, scale, out)
+    if done is not None:
+        return done
+    hq = _heads(q, "q")
+    hk, hv = _heads(k, "k", q), _heads(v, "v", q)
+    (T, H, D), J = q.shape, k.shape[1]
+    if v.shape[1] != J:
+        raise FptqError(-2, f"k has {J} heads, v {v.shape[1]}")
+    _dev(cu, torch.int32, "cu")
+    out = _rows(out, T, H, D, q, "out")
+    _check(lib().fptq_prompt_attention(hq, hk, hv, T, cu.numel() - 1, H, J, D, D ** -0.5 if scale is None else float(scale), _ptr(cu), _ptr(out), _stream()))
+    return out
 
 
 def fptq_set_gemm_map(mode):

@@ -5,6 +5,7 @@
 #include <cstdio>
 #include <mutex>
 
+#include "fptq_attention.h"
 #include "fptq_common.h"
 #include "fptq_testing.h"
 
@@ -162,13 +163,94 @@ static int linear_common(const char *fn, linear_fn force, const void *xq, const 
     return e == hipSuccess ? FPTQ_OK : hip_fail(fn, e);
 }
 
+// ---- attention: what its entry points check alike
+
+static const int64_t MAX_TOKENS = (int64_t)1 << 24, MAX_STRIDE = (int64_t)1 << 24, MAX_HEADS = 4096;
+
+static int check_heads(const char *fn, const fptq_heads *x, const char *name)
+{
+    if (!x || !x->data) {
+        set_error("%s: NULL pointer (%s)", fn, name);
+        return FPTQ_ERR_NULL;
+    }
+    for (int64_t stride : {x->token_stride, x->head_stride}) {
+        if (stride < 0 || stride >= MAX_STRIDE) {
+            set_error("%s: %s has a stride of %lld values, 0 to 2^24 - 8 are served", fn, name, (long long)stride);
+            return FPTQ_ERR_SHAPE;
+        }
+        if (stride % 8) {
+            set_error("%s: the strides of %s must be multiples of 8 values", fn, name);
+            return FPTQ_ERR_ALIGN;
+        }
+    }
+    return check_align(fn, x->data, 16, name);
+}
+
+static int check_attention(const char *fn, int64_t tokens, int64_t sequences, int heads, int kv_heads, int head_dim)
+{
+    if (tokens < 0 || tokens > MAX_TOKENS || sequences < 1 || sequences > MAX_TOKENS || heads < 1 || heads > MAX_HEADS || kv_heads < 1 || heads % kv_heads) {
+        set_error("%s: bad shape tokens=%lld sequences=%lld heads=%d kv_heads=%d", fn, (long long)tokens, (long long)sequences, heads, kv_heads);
+        return FPTQ_ERR_SHAPE;
+    }
+    if (head_dim != 64 && head_dim != 128) {
+        set_error("%s: head_dim must be 64 or 128 (got %d)", fn, head_dim);
+        return FPTQ_ERR_SHAPE;
+    }
+    return FPTQ_OK;
+}
+
+static int check_cache(const char *fn, const fptq_cache *c, int kv_heads, int head_dim, const int32_t *table, int64_t table_width, const int32_t *lengths,
+                       const int32_t *cu, int64_t tokens, int64_t sequences)
+{
+    if (!c || !c->key_codes || !c->value_codes || !c->key_scales || !c->value_scales || !table || !lengths) {
+        set_error("%s: NULL pointer (cache, table or lengths)", fn);
+        return FPTQ_ERR_NULL;
+    }
+    if (c->pages < 1 || c->pages > 0x7fffffff || c->pages > MAX_ELEMS / ((int64_t)kv_heads * PAGE * head_dim) || table_width < 1 || table_width > 1 << 24) {
+        set_error("%s: bad shape pages=%lld table_width=%lld", fn, (long long)c->pages, (long long)table_width);
+        return FPTQ_ERR_SHAPE;
+    }
+    if (!cu && tokens != sequences) {
+        set_error("%s: without cu every sequence has one token (%lld tokens, %lld sequences)", fn, (long long)tokens, (long long)sequences);
+        return FPTQ_ERR_SHAPE;
+    }
+    int rc;
+    if ((rc = check_align(fn, c->key_codes, 16, "key_codes")) || (rc = check_align(fn, c->value_codes, 16, "value_codes")) ||
+        (rc = check_align(fn, c->key_scales, 4, "key_scales")) || (rc = check_align(fn, c->value_scales, 4, "value_scales")) ||
+        (rc = check_align(fn, table, 4, "table")) || (rc = check_align(fn, lengths, 4, "lengths")) || (rc = check_align(fn, cu, 4, "cu")))
+        return rc;
+    return FPTQ_OK;
+}
+
+static int check_scale(const char *fn, float scale)
+{
+    if (!(scale > 0.0f) || !std::isfinite(scale)) {
+        set_error("%s: scale must be finite and > 0", fn);
+        return FPTQ_ERR_VALUE;
+    }
+    return FPTQ_OK;
+}
+
+static Heads heads_of(const fptq_heads *x) { return {(const uint16_t *)x->data, x->token_stride, x->head_stride}; }
+static Cache cache_of(const fptq_cache *c) { return {(uint8_t *)c->key_codes, (uint8_t *)c->value_codes, c->key_scales, c->value_scales, c->pages}; }
+
+// a launch that would have more workgroups than a grid may
+static int launched(const char *fn, hipError_t e)
+{
+    if (e == hipErrorInvalidConfiguration) {
+        set_error("%s: too many tokens, sequences and heads for one call", fn);
+        return FPTQ_ERR_SHAPE;
+    }
+    return e == hipSuccess ? FPTQ_OK : hip_fail(fn, e);
+}
+
 }  // namespace fptq
 
 using namespace fptq;
 
 extern "C" {
 
-int fptq_version(void) { return 200; }
+int fptq_version(void) { return 210; }
 
 int fptq_init(void)
 {
@@ -493,6 +575,88 @@ int fptq_set_gemm_tile(int tile)
     }
     set_gemm_tile(tile);
     return FPTQ_OK;
+}
+
+int fptq_cache_append(const fptq_heads *q, const fptq_heads *k, const fptq_heads *v, int64_t tokens, int64_t sequences, int heads, int kv_heads,
+                      int head_dim, const float *rope, int64_t positions, int rope_dims, int interleaved, const fptq_cache *cache, const int32_t *table,
+                      int64_t table_width, const int32_t *lengths, const int32_t *cu, void *q_out, void *k_out, void *stream)
+{
+    const char *fn = "fptq_cache_append";
+    int rc;
+    if ((rc = check_attention(fn, tokens, sequences, heads, kv_heads, head_dim))) return rc;
+    if (tokens == 0) return FPTQ_OK;             // an empty tensor has no address
+    if ((rc = check_heads(fn, q, "q")) || (rc = check_heads(fn, k, "k")) || (rc = check_heads(fn, v, "v")) ||
+        (rc = check_cache(fn, cache, kv_heads, head_dim, table, table_width, lengths, cu, tokens, sequences)))
+        return rc;
+    if (!q_out || (rope_dims != 0 && !rope)) {
+        set_error("%s: NULL pointer (%s)", fn, q_out ? "rope" : "q_out");
+        return FPTQ_ERR_NULL;
+    }
+    if (rope_dims < 0 || rope_dims > head_dim || rope_dims % 16 || (rope_dims && (positions < 1 || positions > MAX_ELEMS / rope_dims))) {
+        set_error("%s: rope_dims must be a multiple of 16 up to head_dim, positions >= 1 (got %d, %lld)", fn, rope_dims, (long long)positions);
+        return FPTQ_ERR_SHAPE;
+    }
+    if ((rc = check_align(fn, rope, 16, "rope")) || (rc = check_align(fn, q_out, 16, "q_out")) || (rc = check_align(fn, k_out, 16, "k_out"))) return rc;
+    const Sequences s = {cu, lengths, table, (int32_t)sequences, (int32_t)tokens, table_width};
+    return launched(fn, launch_cache_append(heads_of(q), heads_of(k), heads_of(v), s, heads, kv_heads, head_dim, rope, positions, rope_dims, interleaved != 0,
+                                            cache_of(cache), (uint16_t *)q_out, (uint16_t *)k_out, (hipStream_t)stream));
+}
+
+int64_t fptq_cached_attention_scratch_bytes(int64_t tokens, int64_t sequences, int heads, int kv_heads, int head_dim, int64_t table_width)
+{
+    const char *fn = "fptq_cached_attention_scratch_bytes";
+    const int rc = check_attention(fn, tokens, sequences, heads, kv_heads, head_dim);
+    if (rc) return rc;
+    if (table_width < 1 || table_width > 1 << 24) {
+        set_error("%s: bad shape table_width=%lld", fn, (long long)table_width);
+        return FPTQ_ERR_SHAPE;
+    }
+    return cached_attention_scratch_bytes(tokens, sequences, heads, kv_heads, head_dim, table_width);
+}
+
+int fptq_cached_attention(const fptq_heads *q, int64_t tokens, int64_t sequences, int heads, int kv_heads, int head_dim, float scale,
+                          const fptq_cache *cache, const int32_t *table, int64_t table_width, const int32_t *lengths, const int32_t *cu, void *out,
+                          void *scratch, int64_t scratch_bytes, void *stream)
+{
+    const char *fn = "fptq_cached_attention";
+    int rc;
+    if ((rc = check_attention(fn, tokens, sequences, heads, kv_heads, head_dim))) return rc;
+    if (tokens == 0) return FPTQ_OK;
+    if ((rc = check_heads(fn, q, "q")) ||
+        (rc = check_cache(fn, cache, kv_heads, head_dim, table, table_width, lengths, cu, tokens, sequences)) || (rc = check_scale(fn, scale)))
+        return rc;
+    if (!out) {
+        set_error("%s: NULL pointer (out)", fn);
+        return FPTQ_ERR_NULL;
+    }
+    if (scratch_bytes < 0) {
+        set_error("%s: negative scratch_bytes", fn);
+        return FPTQ_ERR_SIZE;
+    }
+    if ((rc = check_align(fn, out, 16, "out")) || (rc = check_align(fn, scratch, 256, "scratch"))) return rc;
+    const Sequences s = {cu, lengths, table, (int32_t)sequences, (int32_t)tokens, table_width};
+    return launched(fn, launch_cached_attention(heads_of(q), s, heads, kv_heads, head_dim, scale, cache_of(cache), (uint16_t *)out, (uint8_t *)scratch,
+                                                scratch_bytes, (hipStream_t)stream));
+}
+
+int fptq_prompt_attention(const fptq_heads *q, const fptq_heads *k, const fptq_heads *v, int64_t tokens, int64_t sequences, int heads, int kv_heads,
+                          int head_dim, float scale, const int32_t *cu, void *out, void *stream)
+{
+    const char *fn = "fptq_prompt_attention";
+    int rc;
+    if ((rc = check_attention(fn, tokens, sequences, heads, kv_heads, head_dim))) return rc;
+    if (tokens == 0) return FPTQ_OK;
+    if ((rc = check_heads(fn, q, "q")) || (rc = check_heads(fn, k, "k")) ||
+        (rc = check_heads(fn, v, "v")) || (rc = check_scale(fn, scale)))
+        return rc;
+    if (!cu || !out) {
+        set_error("%s: NULL pointer (%s)", fn, cu ? "out" : "cu");
+        return FPTQ_ERR_NULL;
+    }
+    if ((rc = check_align(fn, cu, 4, "cu")) || (rc = check_align(fn, out, 16, "out"))) return rc;
+    const Sequences s = {cu, nullptr, nullptr, (int32_t)sequences, (int32_t)tokens, 0};
+    return launched(fn, launch_prompt_attention(heads_of(q), heads_of(k), heads_of(v), s, heads, kv_heads, head_dim, scale, (uint16_t *)out,
+                                                (hipStream_t)stream));
 }
 
 int fptq_unpack(const void *packed, int64_t rows, int64_t K, int8_t *out_int8, void *stream)

@@ -1,0 +1,471 @@
+// Attention over the paged 8-bit cache: a sequence's last tokens (one each in a token loop) against all its keys and values.
+//
+//   o = sum_t p_t v_t / sum_t p_t,   p_t = exp2(c (q . k_t) - m),   c = scale * log2 e,   m the running maximum of c (q . k_t)
+//
+// in one pass over the cache.  What bounds it is the reading of the cache: 2 D bytes a token and kv head, some 2 G operations a byte.
+//
+// A wave takes a page-head (64 tokens of a kv head) at a time.  The query rows that read it (G heads of every new token) are the columns of the matrix
+// instructions, 16 of them or 32, so nothing of the cache is read twice:  S^T = K Q^T and O^T = V^T P^T.  Codes go from memory to registers 16 bytes a
+// lane and are widened to bf16 there, scale included (both exact), two values an instruction; the page's layout is such that each lane's 16 bytes are
+// what the instructions want of it: of keys 16 values of one token; of values the 16 tokens whose scores the lane holds, when row
+// 4 g + i of the b-th 16 of S^T is token 16 g + 4 b + i.  So P^T needs no exchange between lanes and nothing goes through LDS in the loop.
+//
+// P is rounded to bf16 (half a step, 2^-9 of each term); maxima, sums and outputs are fp32.  The accumulators are rescaled only when a maximum has
+// grown by more than 2^8: until then p is at most 256 and loses nothing, being a float.
+//
+// Ragged batches: a unit is a sequence, kv head and 16 or 32 rows.  Units of more pages than an even share of all are cut into equal parts, whose
+// results a second kernel joins.  Everything about lengths is read on the device, so a captured launch serves growing sequences.
+#include "fptq_attention.h"
+
+namespace fptq {
+
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+constexpr int WAVES = 4;                       // of a workgroup; they take every fourth page
+constexpr int MIN_SHARE = 16;                  // pages of a part at least
+constexpr int PARTS = 2048;                    // what all pages are shared out to, about
+
+struct DecodeArgs {
+    Heads q;
+    Sequences seq;
+    Cache cache;
+    uint16_t *out;
+    float *parts;                              // [2 PARTS][rows][D] sums, then [2 PARTS][rows][2] maxima and weights
+    int heads, kv_heads, group;
+    float scale;                               // times log2 e
+};
+
+struct Shape {
+    int tiles, pages;                          // of a sequence: row tiles of each kv head, pages
+};
+template <int ROWS>
+__device__ inline Shape shape_of(const DecodeArgs &a, int b)
+{
+    const int rows = new_tokens(a.seq, b).n * a.group;
+    return {(rows + ROWS - 1) / ROWS, (int)min((int64_t)(length_of(a.seq, b) + PAGE - 1) / PAGE, a.seq.table_width)};
+}
+
+// An even share of all pages, at least MIN_SHARE; without room for parts, everything is one
+template <int ROWS>
+__device__ inline int share(const DecodeArgs &a)
+{
+    if (!a.parts) return 1 << 30;
+    int64_t all = 0;
+    for (int b0 = 0; b0 < a.seq.count; b0 += 64) {
+        const int b = b0 + lane_id();
+        const Shape s = b < a.seq.count ? shape_of<ROWS>(a, b) : Shape{0, 0};
+        all += (int64_t)s.tiles * s.pages;
+    }
+#pragma unroll
+    for (int off = 32; off; off >>= 1) all += __shfl_xor(all, off);
+    all *= a.kv_heads;
+    return (int)min(max((all + PARTS - 1) / PARTS, (int64_t)MIN_SHARE), (int64_t)1 << 30);
+}
+
+struct Unit {
+    int sequence, head, tile, part, parts, slot;      // slot: where the part's results go
+};
+// Item `item` of the list of all parts: first those of units that are cut, then whole units
+template <int ROWS>
+__device__ inline bool find_unit(const DecodeArgs &a, int item, int most, Unit &u)
+{
+    const auto cuts = [&](const Shape &s) { return (s.pages + most - 1) / most; };
+    Found f = find_sequence(a.seq.count, item, [&](int b) {
+        const Shape s = shape_of<ROWS>(a, b);
+        const int n = cuts(s);
+        return n > 1 ? n * s.tiles * a.kv_heads : 0;
+    });
+    u.slot = item;
+    if (f.sequence < 0)
+        f = find_sequence(a.seq.count, f.place, [&](int b) {
+            const Shape s = shape_of<ROWS>(a, b);
+            return cuts(s) > 1 ? 0 : s.tiles * a.kv_heads;
+        });
+    if (f.sequence < 0) return false;
+    const int b = uniform(f.sequence);
+    const Shape s = shape_of<ROWS>(a, b);
+    u.parts = uniform(max(cuts(s), 1));
+    const int place = uniform(f.place), unit = place / u.parts;
+    u.sequence = b, u.part = place % u.parts, u.tile = unit / a.kv_heads, u.head = unit % a.kv_heads;
+    return true;
+}
+
+__device__ inline uint32_t widen(uint32_t codes, float scale, bool high)
+{
+    return __builtin_bit_cast(uint32_t, high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)codes, scale, true)
+                                             : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)codes, scale, false));
+}
+// eight codes to a fragment
+__device__ inline v8bf fragment(uint32_t a, uint32_t b, float scale)
+{
+    return __builtin_bit_cast(v8bf, v4u{widen(a, scale, false), widen(a, scale, true), widen(b, scale, false), widen(b, scale, true)});
+}
+
+// bytes of a word that are e4m3's NaN, as 0xff each
+__device__ inline uint32_t nan_bytes(uint32_t w)
+{
+    const uint32_t t = (w & 0x7f7f7f7fu) + 0x01010101u;       // bit 7 of a byte: its seven bits are all ones
+    return (t >> 7 & 0x01010101u) * 0xffu;
+}
+
+// maximum and sum over the four lanes of a column (16 and 32 lanes away)
+__device__ inline float column_max(float v)
+{
+    const uint32_t u = __float_as_uint(v);
+    const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const uint32_t w = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+    const auto b = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ inline float column_sum(float v)
+{
+    const uint32_t u = __float_as_uint(v);
+    const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const uint32_t w = __float_as_uint(__uint_as_float(a[0]) + __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+constexpr float NONE = -__builtin_inff();
+
+template <int D, int RT>
+__global__ __launch_bounds__(64 * WAVES, 2) void cached_attention_kernel(const DecodeArgs a)
+{
+    constexpr int ROWS = 16 * RT, KB = D / 64, DG = D / 16, PITCH = D + 4;
+    __shared__ __attribute__((aligned(16))) float sums[WAVES][ROWS][PITCH];
+    __shared__ float stats[WAVES][ROWS][2];
+    const int most = share<ROWS>(a);
+    Unit u;
+    if (!find_unit<ROWS>(a, blockIdx.x, most, u)) return;
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
+    const Span span = new_tokens(a.seq, u.sequence);
+    const int begin = uniform(span.begin), n = uniform(span.n), length = uniform(length_of(a.seq, u.sequence));
+    const int pages = (int)min((int64_t)(length + PAGE - 1) / PAGE, a.seq.table_width);
+    const int rows = n * a.group, row0 = u.tile * ROWS;
+
+    // the rows' queries, and how many keys each sees
+    // (32 rows of 128 values leave no registers for them: every page reads them from LDS again)
+    constexpr bool IN_LDS = RT == 2 && D == 128;
+    __shared__ __attribute__((aligned(16))) v8bf shared_q[IN_LDS ? RT * KB * 2 : 1][64];
+    v8bf q[RT][KB][2];
+    int limit[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int row = row0 + 16 * t + col, token = min(row, rows - 1) / a.group, h = min(row, rows - 1) % a.group;
+        limit[t] = row < rows ? max(length - n + 1 + token, 0) : 0;
+        const uint16_t *const from = a.q.p + (int64_t)(begin + token) * a.q.token + (int64_t)(u.head * a.group + h) * a.q.head + g * 16;
+#pragma unroll
+        for (int k = 0; k < KB; ++k)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) q[t][k][s] = __builtin_bit_cast(v8bf, *(const v4u *)(from + k * 64 + s * 8));
+    }
+    if (IN_LDS) {
+        if (wave == 0)
+#pragma unroll
+            for (int i = 0; i < RT * KB * 2; ++i) shared_q[i][lane] = q[i / (KB * 2)][i / 2 % KB][i % 2];
+        __syncthreads();
+    }
+    const int first_token = row0 / a.group, last_token = (min(row0 + ROWS, rows) - 1) / a.group;
+    const int all_see = row0 + ROWS <= rows ? max(length - n + 1 + first_token, 0) : 0;      // keys below it need no mask
+    const int some_see = max(length - n + 1 + last_token, 0);                                // keys from it on nobody sees
+
+    // this part's pages that anybody sees, every fourth one this wave's
+    const int per = (pages + u.parts - 1) / u.parts, from = u.part * per;
+    const int to = min(min(from + per, pages), (some_see + PAGE - 1) / PAGE);
+    const int mine = max((to - from - wave + WAVES - 1) / WAVES, 0);
+    const int32_t *const table = a.seq.table + (int64_t)u.sequence * a.seq.table_width + from + wave;
+
+    v4f o[RT][DG];
+    float m[RT], base[RT], l[RT];                // maxima so far, what is subtracted (0 while there is none), this lane's share of the sums
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        m[t] = NONE, base[t] = 0.0f, l[t] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < DG; ++d) o[t][d] = v4f{0, 0, 0, 0};
+    }
+    const int k_lane = (16 * (col >> 2) + (col & 3)) * 64 + g * 16, v_lane = g * (16 * D) + col * 16;
+
+    for (int i0 = 0; i0 < mine; i0 += 64) {
+        // up to 64 of the wave's pages: a lane looks one up.  A number outside the pool is no page: its tokens are not seen.
+        int id = -1;
+        float ks = 1.0f, vs = 1.0f;
+        if (i0 + lane < mine) {
+            id = table[(i0 + lane) * WAVES];
+            if (id < 0 || id >= a.cache.pages) id = -1;
+            const int64_t at = (int64_t)max(id, 0) * a.kv_heads + u.head;
+            ks = a.cache.ks[at], vs = a.cache.vs[at];
+        }
+        const int count = min(mine - i0, 64);
+        v4u kc[KB][4], vc[DG];
+        auto base_of = [&](int i) { return ((int64_t)max(__builtin_amdgcn_readlane(id, i), 0) * a.kv_heads + u.head) * (PAGE * D); };
+        auto load_keys = [&](int i) {
+            const uint8_t *const p = a.cache.k + base_of(i);
+#pragma unroll
+            for (int k = 0; k < KB; ++k)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) kc[k][b] = *(const v4u *)(p + k_lane + k * (PAGE * 64) + b * 256);
+        };
+        auto load_values = [&](int i) {
+            const uint8_t *const p = a.cache.v + base_of(i);
+#pragma unroll
+            for (int d = 0; d < DG; ++d) vc[d] = *(const v4u *)(p + v_lane + d * 256);
+        };
+        load_keys(0);
+        load_values(0);
+        for (int i = 0; i < count; ++i) {
+            const bool more = i + 1 < count;
+            const bool there = __builtin_amdgcn_readlane(id, i) >= 0;
+            const float key_scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), i));
+            const float value_scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), i));
+            const int position = (from + wave + (i0 + i) * WAVES) * PAGE;
+            v4f s[RT][4];
+            if (IN_LDS) {
+                asm volatile("" ::: "memory");
+#pragma unroll
+                for (int i = 0; i < RT * KB * 2; ++i) q[i / (KB * 2)][i / 2 % KB][i % 2] = shared_q[i][lane];
+            }
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+#pragma unroll
+                for (int t = 0; t < RT; ++t) s[t][b] = v4f{0, 0, 0, 0};
+#pragma unroll
+                for (int k = 0; k < KB; ++k)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const v8bf f = fragment(kc[k][b][2 * h], kc[k][b][2 * h + 1], key_scale);
+#pragma unroll
+                        for (int t = 0; t < RT; ++t) s[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, q[t][k][h], s[t][b], 0, 0, 0);
+                    }
+            }
+            const bool masked = !there || position + PAGE > all_see;
+            if (masked) {
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    const int seen = there ? limit[t] - position - 16 * g : 0;         // of the lane's 16 tokens
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[t][b][e] = 4 * b + e < seen ? s[t][b][e] : NONE;
+                }
+                // what nobody sees may hold anything, and 0 times NaN is NaN
+                const int seen = there ? some_see - position - 16 * g : 0;
+                const v4u keep = {seen >= 4 ? ~0u : seen <= 0 ? 0u : (1u << 8 * seen) - 1u, seen >= 8 ? ~0u : seen <= 4 ? 0u : (1u << 8 * (seen - 4)) - 1u,
+                                  seen >= 12 ? ~0u : seen <= 8 ? 0u : (1u << 8 * (seen - 8)) - 1u, seen >= 16 ? ~0u : seen <= 12 ? 0u : (1u << 8 * (seen - 12)) - 1u};
+#pragma unroll
+                for (int d = 0; d < DG; ++d) vc[d] &= keep;
+                // Nor may a NaN that some rows see reach the others: it is taken out, and the rows that see it are found by a product of indicators.
+                uint32_t bad = 0;
+#pragma unroll
+                for (int d = 0; d < DG; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) bad |= nan_bytes(vc[d][e]);
+                if (__any(bad != 0)) {
+#pragma unroll
+                    for (int d = 0; d < DG; ++d) {
+                        v4u hit;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) hit[e] = nan_bytes(vc[d][e]), vc[d][e] &= ~hit[e], hit[e] &= 0x38383838u;      // 1.0
+#pragma unroll
+                        for (int t = 0; t < RT; ++t) {
+                            const int rows_see = there ? limit[t] - position - 16 * g : 0;
+                            v4f times = {0, 0, 0, 0};
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                v4u see;
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) see[e] = (8 * h + 2 * e < rows_see ? 0x3f80u : 0u) | (8 * h + 2 * e + 1 < rows_see ? 0x3f800000u : 0u);
+                                times = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fragment(hit[2 * h], hit[2 * h + 1], 1.0f), __builtin_bit_cast(v8bf, see), times, 0, 0, 0);
+                            }
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (times[e] > 0.0f) o[t][d][e] = __builtin_nanf("");
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+            }
+            if (more) load_keys(i + 1);
+            uint32_t p[RT][8];
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                float top = s[t][0][0];
+#pragma unroll
+                for (int e = 1; e < 16; ++e) top = fmaxf(top, s[t][e >> 2][e & 3]);
+                top *= a.scale;
+                if (__any(top > m[t] + 8.0f)) {
+                    const float grown = fmaxf(m[t], column_max(top));
+                    const float by = m[t] == NONE ? 0.0f : __builtin_amdgcn_exp2f(m[t] - grown);
+                    m[t] = grown, base[t] = grown == NONE ? 0.0f : grown;
+                    l[t] *= by;
+#pragma unroll
+                    for (int d = 0; d < DG; ++d) o[t][d] *= by;
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1)], a.scale, -base[t]));
+                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1) + 1], a.scale, -base[t]));
+                    l[t] += x + y;
+                    p[t][e] = pack_bf16(x, y);
+                }
+            }
+#pragma unroll
+            for (int d = 0; d < DG; ++d) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const v8bf f = fragment(vc[d][2 * h], vc[d][2 * h + 1], value_scale);
+#pragma unroll
+                    for (int t = 0; t < RT; ++t)
+                        o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, __builtin_bit_cast(v8bf, v4u{p[t][4 * h], p[t][4 * h + 1], p[t][4 * h + 2], p[t][4 * h + 3]}), o[t][d], 0, 0, 0);
+                }
+            }
+            if (more) load_values(i + 1);
+        }
+    }
+
+    // the waves' results, brought to one maximum
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const float sum = column_sum(l[t]);
+        if (g == 0) stats[wave][16 * t + col][0] = m[t], stats[wave][16 * t + col][1] = sum;
+#pragma unroll
+        for (int d = 0; d < DG; ++d) *(v4f *)&sums[wave][16 * t + col][16 * d + 4 * g] = o[t][d];
+    }
+    __syncthreads();
+    constexpr int PER_ROW = D / 8;
+    for (int at = threadIdx.x; at < ROWS * PER_ROW; at += 64 * WAVES) {
+        const int row = at / PER_ROW, d0 = at % PER_ROW * 8;
+        if (row0 + row >= rows) continue;
+        float top = NONE, weight = 0.0f;
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, stats[w][row][0]);
+        v4f x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+        for (int w = 0; w < WAVES; ++w) {
+            // a wave that has seen nothing: zero sums, or NaN where a score was one
+            const float mw = stats[w][row][0], by = mw == NONE ? 1.0f : __builtin_amdgcn_exp2f(mw - top);
+            weight += by * stats[w][row][1];
+            x += by * *(const v4f *)&sums[w][row][d0], y += by * *(const v4f *)&sums[w][row][d0 + 4];
+        }
+        if (u.parts > 1) {
+            float *const to_sums = a.parts + ((int64_t)u.slot * ROWS + row) * D + d0;
+            *(v4f *)to_sums = x, *(v4f *)(to_sums + 4) = y;
+            if (d0 == 0) {
+                float *const to_stats = a.parts + (int64_t)2 * PARTS * ROWS * D + ((int64_t)u.slot * ROWS + row) * 2;
+                to_stats[0] = top, to_stats[1] = weight;
+            }
+        } else {
+            const float r = weight == 0.0f ? 0.0f : 1.0f / weight;          // a row that sees nothing: zeros
+            const int token = begin + (row0 + row) / a.group, h = u.head * a.group + (row0 + row) % a.group;
+            *(v4u *)(a.out + ((int64_t)token * a.heads + h) * D + d0) =
+                v4u{pack_bf16(x[0] * r, x[1] * r), pack_bf16(x[2] * r, x[3] * r), pack_bf16(y[0] * r, y[1] * r), pack_bf16(y[2] * r, y[3] * r)};
+        }
+    }
+}
+
+// Joins a row of a unit that was cut: blockIdx.x the row, blockIdx.y the unit.  The waves take every fourth part.
+template <int D, int RT>
+__global__ __launch_bounds__(64 * WAVES) void join_parts_kernel(const DecodeArgs a)
+{
+    constexpr int ROWS = 16 * RT, E = D / 64;
+    __shared__ float sums[WAVES][D], stats[WAVES][2];
+    const int most = share<ROWS>(a);
+    const Found f = find_sequence(a.seq.count, blockIdx.y, [&](int b) {
+        const Shape s = shape_of<ROWS>(a, b);
+        return s.pages > most ? s.tiles * a.kv_heads : 0;
+    });
+    if (f.sequence < 0) return;
+    const int b = uniform(f.sequence), unit = uniform(f.place), tile = unit / a.kv_heads, head = unit % a.kv_heads;
+    const Shape shape = shape_of<ROWS>(a, b);
+    const int parts = uniform((shape.pages + most - 1) / most);
+    const Span span = new_tokens(a.seq, b);
+    const int row = blockIdx.x, at = tile * ROWS + row;
+    if (at >= uniform(span.n) * a.group) return;
+    // parts of the cut units before this sequence's
+    int before = 0;
+    for (int b0 = 0; b0 < b; b0 += 64) {
+        const int i = b0 + lane_id();
+        const Shape s = i < b ? shape_of<ROWS>(a, i) : Shape{0, 0};
+        before += s.pages > most ? (s.pages + most - 1) / most * s.tiles * a.kv_heads : 0;
+    }
+#pragma unroll
+    for (int off = 32; off; off >>= 1) before += __shfl_xor(before, off);
+    const int slot = uniform(before) + unit * parts;
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+    const float *const from = a.parts + ((int64_t)slot * ROWS + row) * D + lane * E;
+    const float *const stat = a.parts + (int64_t)2 * PARTS * ROWS * D + ((int64_t)slot * ROWS + row) * 2;
+    float x[E] = {}, top = NONE, weight = 0.0f;
+#pragma unroll 8
+    for (int p = wave; p < parts; p += WAVES) {
+        const float mp = stat[(int64_t)p * ROWS * 2], lp = stat[(int64_t)p * ROWS * 2 + 1];
+        const float grown = fmaxf(top, mp);
+        const float old = top == NONE ? 1.0f : __builtin_amdgcn_exp2f(top - grown), by = mp == NONE ? 1.0f : __builtin_amdgcn_exp2f(mp - grown);
+        weight = weight * old + lp * by;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = x[e] * old + from[(int64_t)p * ROWS * D + e] * by;
+        top = grown;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) sums[wave][lane * E + e] = x[e];
+    if (lane == 0) stats[wave][0] = top, stats[wave][1] = weight;
+    __syncthreads();
+    if (threadIdx.x >= D) return;
+    float t = NONE, w = 0.0f, y = 0.0f;
+    for (int i = 0; i < WAVES; ++i) t = fmaxf(t, stats[i][0]);
+    for (int i = 0; i < WAVES; ++i) {
+        const float by = stats[i][0] == NONE ? 1.0f : __builtin_amdgcn_exp2f(stats[i][0] - t);
+        w += by * stats[i][1], y += by * sums[i][threadIdx.x];
+    }
+    const int token = uniform(span.begin) + at / a.group, h = head * a.group + at % a.group;
+    a.out[((int64_t)token * a.heads + h) * D + threadIdx.x] = bf16_rne(w == 0.0f ? 0.0f : y / w);
+}
+
+// Rows of a tile: 16, or 32 where the sequences have more on average
+static int row_tiles(int64_t tokens, int64_t sequences, int group) { return tokens * group > 16 * sequences ? 2 : 1; }
+
+// What the host knows of a launch: units (row tiles of every sequence and kv head) and their pages, as many as there can be
+static int64_t most_units(int64_t tokens, int64_t sequences, int group, int kv_heads, int rows)
+{
+    const int64_t tiles = tokens * group / rows + sequences;        // of n rows: n / rows + 1 at most
+    return (tiles < tokens * group ? tiles : tokens * group) * kv_heads;
+}
+static int64_t most_cut(int64_t units, int64_t table_width)         // parts of cut units: each longer than MIN_SHARE, and than an even share
+{
+    if (table_width <= MIN_SHARE) return 0;
+    const int64_t by_width = units * ((table_width + MIN_SHARE - 1) / MIN_SHARE);
+    return by_width < 2 * PARTS ? by_width : 2 * PARTS;
+}
+
+int64_t cached_attention_scratch_bytes(int64_t tokens, int64_t sequences, int heads, int kv_heads, int head_dim, int64_t table_width)
+{
+    const int group = heads / kv_heads, rows = 16 * row_tiles(tokens, sequences, group);
+    return most_cut(most_units(tokens, sequences, group, kv_heads, rows), table_width) ? (int64_t)2 * PARTS * rows * (head_dim + 2) * 4 : 0;
+}
+
+hipError_t launch_cached_attention(Heads q, const Sequences &s, int heads, int kv_heads, int head_dim, float scale, const Cache &cache, uint16_t *out,
+                                   uint8_t *scratch, int64_t scratch_bytes, hipStream_t stream)
+{
+    const DeviceInfo *info;
+    hipError_t e = device_info(&info);
+    if (e != hipSuccess) return e;
+    const int group = heads / kv_heads, tiles = row_tiles(s.tokens, s.count, group), rows = 16 * tiles;
+    const int64_t units = most_units(s.tokens, s.count, group, kv_heads, rows);
+    const int64_t need = cached_attention_scratch_bytes(s.tokens, s.count, heads, kv_heads, head_dim, s.table_width);
+    const bool cut = need > 0 && scratch && scratch_bytes >= need;
+    DecodeArgs a = {q, s, cache, out, cut ? (float *)scratch : nullptr, heads, kv_heads, group, scale * 1.44269504088896341f};
+    const int64_t grid = units + (cut ? most_cut(units, s.table_width) : 0);
+    if (grid > 1 << 23) return hipErrorInvalidConfiguration;
+    const dim3 threads(64 * WAVES), blocks((unsigned)grid);
+    if (head_dim == 128)
+        tiles == 1 ? cached_attention_kernel<128, 1><<<blocks, threads, 0, stream>>>(a) : cached_attention_kernel<128, 2><<<blocks, threads, 0, stream>>>(a);
+    else
+        tiles == 1 ? cached_attention_kernel<64, 1><<<blocks, threads, 0, stream>>>(a) : cached_attention_kernel<64, 2><<<blocks, threads, 0, stream>>>(a);
+    if (cut) {
+        const dim3 joins((unsigned)rows, (unsigned)(units < PARTS ? units : PARTS));
+        if (head_dim == 128)
+            tiles == 1 ? join_parts_kernel<128, 1><<<joins, threads, 0, stream>>>(a) : join_parts_kernel<128, 2><<<joins, threads, 0, stream>>>(a);
+        else
+            tiles == 1 ? join_parts_kernel<64, 1><<<joins, threads, 0, stream>>>(a) : join_parts_kernel<64, 2><<<joins, threads, 0, stream>>>(a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace fptq

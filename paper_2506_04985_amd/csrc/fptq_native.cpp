@@ -7,6 +7,7 @@
 // contiguous or not on the device, a buffer too small, an error of the library): then the wrapper goes on in Python, which
 // raises what there is to raise.  A failing library call launches nothing, so it can be repeated.  Nothing is kept between calls.
 #include <array>
+#include <cmath>
 #include <initializer_list>
 
 #include <torch/extension.h>
@@ -82,7 +83,7 @@ bool truth(PyObject *o)
 struct Output {
     PyObject *given = nullptr;       // the caller's, who holds it
     at::Tensor made;
-    std::array<int64_t, 2> shape = {0, 1};
+    std::array<int64_t, 3> shape = {0, 1, 1};
     int dims = 0;
     at::ScalarType type = at::kByte;
     at::Device device = at::kCPU;
@@ -331,9 +332,132 @@ PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// bf16 [tokens, heads, head_dim], any strides but the last
+fptq_heads heads(PyObject *o, std::array<int64_t, 3> &shape)
+{
+    const at::Tensor &t = device_tensor(o);
+    if (t.scalar_type() != at::kBFloat16 || t.dim() != 3 || t.stride(2) != 1) throw Slow();
+    shape = {t.size(0), t.size(1), t.size(2)};
+    return {t.data_ptr(), shape[0] > 1 ? t.stride(0) : 0, shape[1] > 1 ? t.stride(1) : 0};
+}
+
+// a caller's output of at least n contiguous bf16 values
+Output rows(PyObject *o, std::initializer_list<int64_t> sizes, const at::Tensor &like)
+{
+    int64_t n = 1;
+    for (int64_t s : sizes) n *= s;
+    if (o != Py_None && input(o, at::kBFloat16).numel() < n) throw Slow();
+    return Output(o, sizes, at::kBFloat16, like);
+}
+
+// (key_codes, value_codes, key_scales, value_scales, table, lengths, cu) and what they say of the sequences
+struct Paged {
+    fptq_cache cache;
+    int64_t sequences, width;
+    const int32_t *table, *lengths, *cu;
+    int kv_heads;
+    Paged(PyObject *const *a, int64_t D)
+    {
+        const at::Tensor &kc = input(a[0], at::kByte), &vc = input(a[1], at::kByte), &ks = input(a[2], at::kFloat), &vs = input(a[3], at::kFloat);
+        const at::Tensor &t = input(a[4], at::kInt), &l = input(a[5], at::kInt);
+        sequences = l.numel();
+        if (kc.dim() != 3 || kc.size(2) != 64 * D || vc.sizes() != kc.sizes() || ks.numel() != kc.size(0) * kc.size(1) || vs.numel() != ks.numel()) throw Slow();
+        if (t.dim() != 2 || t.size(0) != sequences) throw Slow();
+        if (a[6] != Py_None && input(a[6], at::kInt).numel() != sequences + 1) throw Slow();
+        cache = {kc.data_ptr(), vc.data_ptr(), (float *)ks.data_ptr(), (float *)vs.data_ptr(), kc.size(0)};
+        width = t.size(1), kv_heads = (int)kc.size(1);
+        table = (const int32_t *)t.data_ptr(), lengths = (const int32_t *)l.data_ptr(), cu = (const int32_t *)input_or_null(a[6], at::kInt);
+    }
+};
+
+float scale_of(PyObject *o, int64_t D) { return o == Py_None ? (float)(1.0 / std::sqrt((double)D)) : number(o); }
+
+// (q, k, v, rope, key_codes, value_codes, key_scales, value_scales, table, lengths, cu, interleaved, want_k, q_out, k_out)
+PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 15, [&]() -> PyObject * {
+        std::array<int64_t, 3> s, sk, sv;
+        const fptq_heads q = heads(a[0], s), k = heads(a[1], sk), v = heads(a[2], sv);
+        const auto [T, H, D] = s;
+        if (sk != sv || sk[0] != T || sk[2] != D) throw Slow();
+        const Paged p(a + 4, D);
+        if (p.kv_heads != sk[1]) throw Slow();
+        const float *rope = nullptr;
+        int64_t positions = 0, rope_dims = 0;
+        if (a[3] != Py_None) {
+            const at::Tensor &r = input(a[3], at::kFloat);
+            if (r.dim() != 3 || r.size(1) != 2) throw Slow();
+            rope = (const float *)r.data_ptr(), positions = r.size(0), rope_dims = 2 * r.size(2);
+            if (rope_dims > D) throw Slow();
+        }
+        const int interleaved = truth(a[11]), dims[3] = {(int)H, (int)sk[1], (int)D};
+        const at::Tensor &like = THPVariable_Unpack(a[0]);
+        Output q_out = rows(a[13], {T, H, D}, like), k_out;
+        if (a[14] != Py_None || truth(a[12])) k_out = rows(a[14], {T, sk[1], D}, like);
+        const int64_t tokens = T;
+        void *const st = where().stream;
+        launch({&q_out, &k_out}, [&] {
+            return fptq_cache_append(&q, &k, &v, tokens, p.sequences, dims[0], dims[1], dims[2], rope, positions, (int)rope_dims, interleaved, &p.cache, p.table,
+                                     p.width, p.lengths, p.cu, q_out.ptr, k_out.ptr, st);
+        });
+        return tuple({&q_out, &k_out});
+    });
+}
+
+// (q, key_codes, value_codes, key_scales, value_scales, table, lengths, cu, scale, out, scratch)
+PyObject *cached_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 11, [&]() -> PyObject * {
+        std::array<int64_t, 3> s;
+        const fptq_heads q = heads(a[0], s);
+        const Paged p(a + 1, s[2]);
+        const float scale = scale_of(a[8], s[2]);
+        const at::Tensor &like = THPVariable_Unpack(a[0]);
+        Output out = rows(a[9], {s[0], s[1], s[2]}, like), room;
+        const Where w = where();
+        void *const st = w.stream;
+        const int64_t tokens = s[0];
+        const int dims[3] = {(int)s[1], p.kv_heads, (int)s[2]};
+        if (a[10] != Py_None) {
+            input(a[10], at::kByte);
+            room = Output(a[10], {}, at::kByte, like);
+        } else if (like.device().index() == w.device) {      // handed back when the call returns: it has to come from the stream of the launch
+            const int64_t bytes = without_gil([&] { return fptq_cached_attention_scratch_bytes(tokens, p.sequences, dims[0], dims[1], dims[2], p.width); });
+            if (bytes < 0) throw Slow();
+            if (bytes > 0) room = Output(Py_None, {bytes}, at::kByte, like);
+        }
+        launch({&out, &room}, [&] {
+            return fptq_cached_attention(&q, tokens, p.sequences, dims[0], dims[1], dims[2], scale, &p.cache, p.table, p.width, p.lengths, p.cu, out.ptr,
+                                         room.ptr, room.numel, st);
+        });
+        return out.take();
+    });
+}
+
+// (q, k, v, cu, scale, out)
+PyObject *prompt_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 6, [&]() -> PyObject * {
+        std::array<int64_t, 3> s, sk, sv;
+        const fptq_heads q = heads(a[0], s), k = heads(a[1], sk), v = heads(a[2], sv);
+        if (sk != sv || sk[0] != s[0] || sk[2] != s[2]) throw Slow();
+        const at::Tensor &cu = input(a[3], at::kInt);
+        const float scale = scale_of(a[4], s[2]);
+        Output out = rows(a[5], {s[0], s[1], s[2]}, THPVariable_Unpack(a[0]));
+        const int64_t tokens = s[0], sequences = cu.numel() - 1;
+        const int dims[3] = {(int)s[1], (int)sk[1], (int)s[2]};
+        void *const st = where().stream;
+        launch({&out}, [&] {
+            return fptq_prompt_attention(&q, &k, &v, tokens, sequences, dims[0], dims[1], dims[2], scale, (const int32_t *)cu.data_ptr(), out.ptr, st);
+        });
+        return out.take();
+    });
+}
+
 #define FPTQ_FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FPTQ_FAST(pack_weights), FPTQ_FAST(weight_row_sums), FPTQ_FAST(quantize_act), FPTQ_FAST(quantize_act_dynamic),
-                         FPTQ_FAST(residual_norm_quantize), FPTQ_FAST(linear), {nullptr, nullptr, 0, nullptr}};
+                         FPTQ_FAST(residual_norm_quantize), FPTQ_FAST(linear), FPTQ_FAST(cache_append), FPTQ_FAST(cached_attention),
+                         FPTQ_FAST(prompt_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

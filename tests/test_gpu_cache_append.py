@@ -1,0 +1,195 @@
+"""fptq_cache_append against the oracle in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from attention_util import PAGE, device, host, paged, projection, starts
+from oracle import attention as oracle
+from paper_2506_04985_amd import binding as fptq
+
+pytestmark = pytest.mark.gpu
+
+
+def rope_table(positions, rope_dims, base=10000.0):
+    angle = np.arange(positions)[:, None] * base ** (-np.arange(0, rope_dims, 2) / rope_dims)
+    return np.stack([np.cos(angle), np.sin(angle)], 1).astype(np.float32)
+
+
+def run(new, before, H, J, D, rope_dims, interleaved, seed=0, want_k=True, with_cu=True, spread=1.0, poison=True, change=None):
+    """Appends `new` tokens of every sequence behind `before` ones of random codes and checks every byte of the cache, the scales and the rotated rows."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rng = np.random.default_rng(seed)
+    q, k, v = projection(g, sum(new), H, J, D, spread)
+    if change:
+        change(q, k, v)
+    lengths = [a + b for a, b in zip(new, before)]
+    table, pool = paged(lengths, seed=seed)
+    codes = rng.integers(0, 256, (2, pool, J, PAGE, D), dtype=np.uint8)
+    codes[(codes & 127) == 127] ^= 1
+    scales = np.exp2(rng.integers(-9, -6, (2, pool, J))).astype(np.float32)
+    flat = [np.stack([[f(x) for x in page] for page in c]) for f, c in zip((oracle.keys_page, oracle.values_page), codes)]
+    cache = fptq.Cache(*(torch.from_numpy(np.ascontiguousarray(x)).cuda() for x in (*flat, scales[0], scales[1])))
+    rope = rope_table(max(lengths), rope_dims) if rope_dims else None
+    q_out, k_out = fptq.fptq_cache_append(q, k, v, None if rope is None else torch.from_numpy(rope).cuda(), cache, device(table), device(lengths),
+                                          device(starts(new)) if with_cu else None, interleaved=interleaved, want_k=want_k)
+    assert want_k or k_out is None
+    exact = {"q": host(q).copy(), "k": host(k).copy(), "v": host(v)}
+    slack = {"q": np.zeros_like(exact["q"]), "k": np.zeros_like(exact["k"]), "v": np.zeros_like(exact["v"])}
+    got_codes = [np.stack([[f(x, D) for x in page] for page in t.cpu().numpy()])
+                 for f, t in ((oracle.from_keys_page, cache.key_codes), (oracle.from_values_page, cache.value_codes))]
+    got_scales = [cache.key_scales.cpu().numpy(), cache.value_scales.cpu().numpy()]
+    touched = np.zeros((2, pool, J, PAGE), bool)
+    values = oracle.e4m3_values()
+    for b, (s, e) in enumerate(zip(starts(new), starts(new)[1:])):
+        for i in range(s, e):
+            if rope is not None:
+                c = rope[before[b] + i - s].astype(np.float64)
+                for name in ("q", "k"):
+                    size = oracle.rotate(np.abs(exact[name][i]), np.abs(c[0]), -np.abs(c[1]), interleaved)       # |x1 c| + |x2 s|, and a lower one
+                    other = oracle.rotate(np.abs(exact[name][i]), np.abs(c[0]), np.abs(c[1]), interleaved)
+                    slack[name][i] = 2 * 2.0 ** -24 * np.maximum(size, other)       # two products and a sum, in fp32
+                    exact[name][i] = oracle.rotate(exact[name][i], c[0], c[1], interleaved)
+        at = before[b]
+        while at < lengths[b]:
+            page, first = table[b, at // PAGE], at % PAGE
+            n = min(PAGE - first, lengths[b] - at)
+            rows = slice(s + at - before[b], s + at - before[b] + n)
+            for which, name in enumerate("kv"):
+                for j in range(J):
+                    new_rows, off = exact[name][rows, j], slack[name][rows, j]
+                    older = values[codes[which, page, j, :first]] * float(scales[which, page, j])
+                    x, scale = oracle.append_page(older, float(scales[which, page, j]), first, new_rows)
+                    got = got_scales[which][page, j]
+                    if got != scale:        # the largest value is within the slack of where the scale steps
+                        largest = np.abs(new_rows[np.isfinite(new_rows)]).max()
+                        assert got == oracle.scale_for(largest + off.max()) or got == oracle.scale_for(largest - off.max()), (got, scale)
+                        scale = float(got)
+                    y = values[got_codes[which][page, j, :first + n]] * scale
+                    finite = np.isfinite(x)
+                    assert np.array_equal(finite, np.isfinite(y))
+                    if scale == float(scales[which, page, j]):
+                        np.testing.assert_array_equal(got_codes[which][page, j, :first], codes[which, page, j, :first])
+                    wide = np.concatenate([np.zeros((first, D)), off])
+                    far = np.abs(y - x) <= np.maximum(2.0 ** -4 * np.abs(x), 2.0 ** -10 * scale) + 1.01 * wide       # half a step, of the subnormals 2^-10
+                    assert far[finite].all()
+                    if rope is None or name == "v":
+                        one_nan = lambda c: np.where(c & 127 == 127, 127, c)           # either sign of it is NaN
+                        np.testing.assert_array_equal(one_nan(got_codes[which][page, j, first:first + n]), one_nan(oracle.e4m3(new_rows / scale)))
+                    touched[which, page, j, :first + n] = True
+            at += n
+    for which in range(2):
+        np.testing.assert_array_equal(np.where(touched[which][..., None], 0, got_codes[which]), np.where(touched[which][..., None], 0, codes[which]))
+        idle = ~touched[which].any(2)
+        np.testing.assert_array_equal(got_scales[which][idle], scales[which][idle])
+    for name, out in (("q", q_out), ("k", k_out)):
+        if out is not None:
+            x = exact[name]
+            finite = np.isfinite(x)
+            y = host(out)
+            assert np.array_equal(finite, np.isfinite(y))
+            assert (np.abs(y - x)[finite] <= (2.0 ** -8 * np.abs(x) + 1.01 * slack[name] + 1e-38)[finite]).all()
+    return cache, q_out, k_out
+
+
+@pytest.mark.parametrize("H,J,D", [(4, 2, 128), (3, 3, 64), (20, 1, 64), (9, 1, 128)])
+@pytest.mark.parametrize("before", [[0], [63, 64, 65], [5, 0, 127, 1000]])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_one_token_each(before, H, J, D, interleaved):
+    run([1] * len(before), before, H, J, D, D, interleaved, seed=H, with_cu=False)
+    run([1] * len(before), before, H, J, D, D, interleaved, seed=H + 1, want_k=False)
+
+
+@pytest.mark.parametrize("rope_dims", [0, 16, 32, 48, 64])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("new,before", [([5, 0, 1], [3, 9, 63]), ([130], [0]), ([63, 65, 64], [1, 64, 0]), ([200, 17], [40, 50])])
+def test_part_of_the_head_and_ragged_tokens(new, before, rope_dims, interleaved):
+    run(new, before, 4, 2, 64, rope_dims, interleaved, seed=rope_dims)
+
+
+@pytest.mark.parametrize("rope_dims", [32, 128])
+def test_wide_heads(rope_dims):
+    run([70, 3, 140], [10, 0, 60], 5, 5, 128, rope_dims, False, seed=2)
+    run([70, 3, 140], [10, 0, 60], 6, 2, 128, rope_dims, True, seed=3)
+
+
+@pytest.mark.parametrize("spread", [0.0, 1e-4, 300.0])
+def test_scales(spread):
+    """Zeros (the smallest scale in a new page, the older one in another), values far below the older ones and far above them."""
+    run([3, 3, 64], [0, 60, 5], 2, 2, 64, 0, False, seed=4, spread=spread)
+    run([3, 3, 64], [0, 60, 5], 2, 2, 128, 128, False, seed=4, spread=spread)
+
+
+def test_largest_values_on_the_step():
+    """448 s exactly takes the scale s, the next bf16 value the double."""
+    def change(q, k, v):
+        k.clamp_(-1, 1), v.clamp_(-1, 1)
+        k[0, 0, 0], k[0, 1, 5] = 1.75, -1.7578125
+        v[0, 0, 3], v[0, 1, 63] = -3.5, 3.515625
+    cache, _, _ = run([64], [0], 2, 2, 64, 0, False, seed=5, change=change)
+    assert sorted(cache.key_scales.flatten().tolist()).count(2.0 ** -8) >= 1
+
+
+def test_values_that_are_not_finite():
+    def change(q, k, v):
+        k[2, 0, 1], k[3, 1, 2], v[1, 0, 60], v[4, 1, 0] = float("nan"), float("inf"), float("-inf"), float("nan")
+    run([6], [70], 2, 2, 64, 0, False, seed=6, change=change)
+
+
+def test_pages_outside_the_pool_and_positions_outside_the_tables():
+    """Nothing is written there; rows outside the rotation's table are NaN, the others as ever."""
+    g = torch.Generator(device="cuda").manual_seed(7)
+    q, k, v = projection(g, 6, 2, 1, 64)
+    cache = fptq.Cache.empty(3, 1, 64)
+    for t in (cache.key_codes, cache.value_codes, cache.key_scales, cache.value_scales):
+        t.fill_(3)
+    rope = torch.from_numpy(rope_table(100, 64)).cuda()
+    table = device([[-1, 3], [0x7FFFFFFF, -0x80000000], [0, 1]])
+    # positions 62, 63 | 64, 65 of bad pages; position -1 of a length that does not count its token; 128: past the table
+    q_out, k_out = fptq.fptq_cache_append(q, k, v, rope, cache, table, device([66, 0, 129]), device([0, 4, 5, 6]), want_k=True)
+    assert (cache.key_codes == 3).all() and (cache.value_codes == 3).all() and (cache.key_scales == 3).all() and (cache.value_scales == 3).all()
+    assert torch.isfinite(q_out[:4]).all() and torch.isfinite(k_out[:4]).all()
+    assert torch.isnan(q_out[4:]).all() and torch.isnan(k_out[4:]).all()
+
+
+def test_native_and_python_binding_agree(monkeypatch):
+    first = run([5, 70], [60, 3], 4, 2, 128, 128, False, seed=8)
+    monkeypatch.setattr(fptq, "_native", None)
+    second = run([5, 70], [60, 3], 4, 2, 128, 128, False, seed=8)
+    assert torch.equal(first[1], second[1]) and torch.equal(first[2], second[2]) and torch.equal(first[0].key_codes, second[0].key_codes)
+
+
+def test_replays_of_a_captured_token_step():
+    """A captured append and attention, fed token by token: the cache and the outputs are those of eager calls on another cache."""
+    H, J, D, B = 4, 2, 64, 3
+    g = torch.Generator(device="cuda").manual_seed(9)
+    rope = torch.from_numpy(rope_table(400, D)).cuda()
+    caches = [fptq.Cache.empty(12, J, D) for _ in range(2)]
+    for c in caches:
+        for t in (c.key_codes, c.value_codes, c.key_scales, c.value_scales):
+            t.zero_()
+    table = device(np.arange(12).reshape(B, 4))
+    lengths = device([0, 61, 5])
+    qkv = torch.empty((B, (H + 2 * J) * D), dtype=torch.bfloat16, device="cuda")
+    q, k, v = (x.unflatten(1, (-1, D)) for x in qkv.split([H * D, J * D, J * D], 1))
+    out = torch.empty((B, H, D), dtype=torch.bfloat16, device="cuda")
+
+    def step(cache, to):
+        rotated, _ = fptq.fptq_cache_append(q, k, v, rope, cache, table, lengths)
+        return fptq.fptq_cached_attention(rotated, cache, table, lengths, out=to)
+
+    fptq.fptq_init()
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        step(caches[0], out)
+    for _ in range(8):
+        qkv.copy_(torch.randn(qkv.shape, device="cuda", generator=g).to(torch.bfloat16))
+        lengths += 1
+        want = step(caches[1], None)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        assert torch.equal(caches[0].key_codes, caches[1].key_codes) and torch.equal(caches[0].value_codes, caches[1].value_codes)
+        assert torch.equal(caches[0].key_scales, caches[1].key_scales)
