@@ -45,6 +45,18 @@ __device__ inline int lane_id() { return __builtin_amdgcn_mbcnt_hi(~0u, __builti
 
 __device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// sums over the lanes up to each one, in row shifts and broadcasts of rows' last lanes (__shfl_up's way through LDS takes six times as long)
+__device__ inline int wave_prefix(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);      // row_shr:1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);      // row_bcast:15 to rows 1 and 3, row_bcast:31 to rows 2 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+    return v;
+}
+
 // Of a list that holds count(b) items of every sequence b, one sequence after the other: the sequence that item `item` belongs to (uniform over
 // the wave) and the item's place among that sequence's, or -1 and the items left over if the list is shorter.  64 sequences a step.
 struct Found {
@@ -55,13 +67,7 @@ __device__ inline Found find_sequence(int sequences, int item, Count count)
 {
     const int lane = lane_id();
     for (int b0 = 0; b0 < sequences; b0 += 64) {
-        const int own = b0 + lane < sequences ? count(b0 + lane) : 0;
-        int upto = own;
-#pragma unroll
-        for (int off = 1; off < 64; off *= 2) {
-            const int below = __shfl_up(upto, off);
-            upto += lane >= off ? below : 0;
-        }
+        const int own = b0 + lane < sequences ? count(b0 + lane) : 0, upto = wave_prefix(own);
         const int all = __builtin_amdgcn_readlane(upto, 63);
         if (item < all) {
             const int at = __builtin_ctzll(__ballot(item < upto));

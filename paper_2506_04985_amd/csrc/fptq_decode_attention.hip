@@ -42,51 +42,68 @@ struct Shape {
 template <int ROWS>
 __device__ inline Shape shape_of(const DecodeArgs &a, int b)
 {
+    if (b >= a.seq.count) return {0, 0};
     const int rows = new_tokens(a.seq, b).n * a.group;
     return {(rows + ROWS - 1) / ROWS, (int)min((int64_t)(length_of(a.seq, b) + PAGE - 1) / PAGE, a.seq.table_width)};
 }
 
-// An even share of all pages, at least MIN_SHARE; without room for parts, everything is one
+// How the pages are shared out: units of more than `most` pages, an even share of all and at least MIN_SHARE, are cut into equal parts.  Every wave
+// finds this out for itself, 64 sequences at a time; the shapes of the first 64 stay in its lanes.
 template <int ROWS>
-__device__ inline int share(const DecodeArgs &a)
-{
-    if (!a.parts) return 1 << 30;
-    int64_t all = 0;
-    for (int b0 = 0; b0 < a.seq.count; b0 += 64) {
-        const int b = b0 + lane_id();
-        const Shape s = b < a.seq.count ? shape_of<ROWS>(a, b) : Shape{0, 0};
-        all += (int64_t)s.tiles * s.pages;
+struct Shares {
+    const DecodeArgs &a;
+    Shape first;
+    int most;
+    __device__ explicit Shares(const DecodeArgs &args) : a(args), first(shape_of<ROWS>(args, lane_id())), most(1 << 30)
+    {
+        if (!a.parts) return;
+        double all = (double)first.tiles * first.pages;        // exact: below 2^53
+        for (int b0 = 64; b0 < a.seq.count; b0 += 64) {
+            const Shape s = shape_of<ROWS>(a, b0 + lane_id());
+            all += (double)s.tiles * s.pages;
+        }
+        all = wave_sum(all) * a.kv_heads;
+        most = uniform((int)fmin(fmax(ceil(all * (1.0 / PARTS)), (double)MIN_SHARE), 0x1p30));
     }
-#pragma unroll
-    for (int off = 32; off; off >>= 1) all += __shfl_xor(all, off);
-    all *= a.kv_heads;
-    return (int)min(max((all + PARTS - 1) / PARTS, (int64_t)MIN_SHARE), (int64_t)1 << 30);
-}
+    __device__ Shape shape(int b) const { return b < 64 ? first : shape_of<ROWS>(a, b); }      // of sequence b, a lane's own in its group of 64
+    __device__ Shape at(int b) const                                                           // of any, for all lanes
+    {
+        if (b >= 64) return shape_of<ROWS>(a, b);
+        return {__builtin_amdgcn_readlane(first.tiles, b), __builtin_amdgcn_readlane(first.pages, b)};
+    }
+    __device__ int cuts(const Shape &s) const { return (s.pages + most - 1) / most; }
+};
 
 struct Unit {
     int sequence, head, tile, part, parts, slot;      // slot: where the part's results go
 };
 // Item `item` of the list of all parts: first those of units that are cut, then whole units
 template <int ROWS>
-__device__ inline bool find_unit(const DecodeArgs &a, int item, int most, Unit &u)
+__device__ inline bool find_unit(const DecodeArgs &a, int item, Unit &u)
 {
-    const auto cuts = [&](const Shape &s) { return (s.pages + most - 1) / most; };
-    Found f = find_sequence(a.seq.count, item, [&](int b) {
-        const Shape s = shape_of<ROWS>(a, b);
-        const int n = cuts(s);
-        return n > 1 ? n * s.tiles * a.kv_heads : 0;
-    });
     u.slot = item;
+    if (!a.parts && !a.seq.cu) {                      // as many units of every sequence, which it takes no lengths to know
+        const int tiles = (a.group + ROWS - 1) / ROWS, unit = item % (tiles * a.kv_heads);
+        u.sequence = item / (tiles * a.kv_heads), u.tile = unit / a.kv_heads, u.head = unit % a.kv_heads, u.part = 0, u.parts = 1;
+        return u.sequence < a.seq.count;
+    }
+    const Shares<ROWS> shares(a);
+    Found f = {-1, item};
+    if (a.parts)
+        f = find_sequence(a.seq.count, item, [&](int b) {
+            const Shape s = shares.shape(b);
+            const int n = shares.cuts(s);
+            return n > 1 ? n * s.tiles * a.kv_heads : 0;
+        });
     if (f.sequence < 0)
         f = find_sequence(a.seq.count, f.place, [&](int b) {
-            const Shape s = shape_of<ROWS>(a, b);
-            return cuts(s) > 1 ? 0 : s.tiles * a.kv_heads;
+            const Shape s = shares.shape(b);
+            return shares.cuts(s) > 1 ? 0 : s.tiles * a.kv_heads;
         });
     if (f.sequence < 0) return false;
-    const int b = uniform(f.sequence);
-    const Shape s = shape_of<ROWS>(a, b);
-    u.parts = uniform(max(cuts(s), 1));
-    const int place = uniform(f.place), unit = place / u.parts;
+    const int b = uniform(f.sequence), place = uniform(f.place);
+    u.parts = uniform(max(shares.cuts(shares.at(b)), 1));
+    const int unit = place / u.parts;
     u.sequence = b, u.part = place % u.parts, u.tile = unit / a.kv_heads, u.head = unit % a.kv_heads;
     return true;
 }
@@ -127,6 +144,15 @@ __device__ inline float column_sum(float v)
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// maximum over 16 lanes
+__device__ inline float row_max(float v)
+{
+    v = fmaxf(v, __uint_as_float(other_lane<8>(__float_as_uint(v))));
+    v = fmaxf(v, __uint_as_float(other_lane<4>(__float_as_uint(v))));
+    v = fmaxf(v, __uint_as_float(other_lane<2>(__float_as_uint(v))));
+    return fmaxf(v, __uint_as_float(other_lane<1>(__float_as_uint(v))));
+}
+
 constexpr float NONE = -__builtin_inff();
 
 template <int D, int RT>
@@ -135,9 +161,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cached_attention_kernel(const D
     constexpr int ROWS = 16 * RT, KB = D / 64, DG = D / 16, PITCH = D + 4;
     __shared__ __attribute__((aligned(16))) float sums[WAVES][ROWS][PITCH];
     __shared__ float stats[WAVES][ROWS][2];
-    const int most = share<ROWS>(a);
     Unit u;
-    if (!find_unit<ROWS>(a, blockIdx.x, most, u)) return;
+    if (!find_unit<ROWS>(a, blockIdx.x, u)) return;
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const Span span = new_tokens(a.seq, u.sequence);
     const int begin = uniform(span.begin), n = uniform(span.n), length = uniform(length_of(a.seq, u.sequence));
@@ -174,25 +199,27 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cached_attention_kernel(const D
     const int per = (pages + u.parts - 1) / u.parts, from = u.part * per;
     const int to = min(min(from + per, pages), (some_see + PAGE - 1) / PAGE);
     const int mine = max((to - from - wave + WAVES - 1) / WAVES, 0);
-    const int32_t *const table = a.seq.table + (int64_t)u.sequence * a.seq.table_width + from + wave;
+    const int32_t *const table = a.seq.table + (int64_t)u.sequence * a.seq.table_width;
 
     v4f o[RT][DG];
-    float m[RT], base[RT], l[RT];                // maxima so far, what is subtracted (0 while there is none), this lane's share of the sums
+    float m[RT], l[RT];                          // maxima so far, this lane's share of the sums
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        m[t] = NONE, base[t] = 0.0f, l[t] = 0.0f;
+        m[t] = NONE, l[t] = 0.0f;
 #pragma unroll
         for (int d = 0; d < DG; ++d) o[t][d] = v4f{0, 0, 0, 0};
     }
     const int k_lane = (16 * (col >> 2) + (col & 3)) * 64 + g * 16, v_lane = g * (16 * D) + col * 16;
 
+    // up to 64 of the wave's pages at a time: a lane looks one up (the first of them while the length is on its way)
+    const auto look_up = [&](int i0) { return table[min((int64_t)(from + wave + (i0 + lane) * WAVES), a.seq.table_width - 1)]; };
+    int id = look_up(0);
     for (int i0 = 0; i0 < mine; i0 += 64) {
-        // up to 64 of the wave's pages: a lane looks one up.  A number outside the pool is no page: its tokens are not seen.
-        int id = -1;
+        if (i0) id = look_up(i0);
+        // A number outside the pool is no page: its tokens are not seen.
+        if (i0 + lane >= mine || id < 0 || id >= a.cache.pages) id = -1;
         float ks = 1.0f, vs = 1.0f;
         if (i0 + lane < mine) {
-            id = table[(i0 + lane) * WAVES];
-            if (id < 0 || id >= a.cache.pages) id = -1;
             const int64_t at = (int64_t)max(id, 0) * a.kv_heads + u.head;
             ks = a.cache.ks[at], vs = a.cache.vs[at];
         }
@@ -296,15 +323,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cached_attention_kernel(const D
                 if (__any(top > m[t] + 8.0f)) {
                     const float grown = fmaxf(m[t], column_max(top));
                     const float by = m[t] == NONE ? 0.0f : __builtin_amdgcn_exp2f(m[t] - grown);
-                    m[t] = grown, base[t] = grown == NONE ? 0.0f : grown;
+                    m[t] = grown;
                     l[t] *= by;
 #pragma unroll
                     for (int d = 0; d < DG; ++d) o[t][d] *= by;
                 }
+                const float base = m[t] == NONE ? 0.0f : m[t];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1)], a.scale, -base[t]));
-                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1) + 1], a.scale, -base[t]));
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1)], a.scale, -base));
+                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1) + 1], a.scale, -base));
                     l[t] += x + y;
                     p[t][e] = pack_bf16(x, y);
                 }
@@ -361,61 +389,79 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cached_attention_kernel(const D
     }
 }
 
-// Joins a row of a unit that was cut: blockIdx.x the row, blockIdx.y the unit.  The waves take every fourth part.
+// Joins the parts of a unit that was cut, a row to a wave, or to the four waves of a workgroup, which then take every fourth part.  blockIdx.y: the unit.
 template <int D, int RT>
-__global__ __launch_bounds__(64 * WAVES) void join_parts_kernel(const DecodeArgs a)
+__global__ __launch_bounds__(64 * WAVES) void join_parts_kernel(const DecodeArgs a, int waves_a_row)
 {
     constexpr int ROWS = 16 * RT, E = D / 64;
     __shared__ float sums[WAVES][D], stats[WAVES][2];
-    const int most = share<ROWS>(a);
+    const Shares<ROWS> shares(a);
+    const auto cut = [&](const Shape &s) { return s.pages > shares.most; };
     const Found f = find_sequence(a.seq.count, blockIdx.y, [&](int b) {
-        const Shape s = shape_of<ROWS>(a, b);
-        return s.pages > most ? s.tiles * a.kv_heads : 0;
+        const Shape s = shares.shape(b);
+        return cut(s) ? s.tiles * a.kv_heads : 0;
     });
     if (f.sequence < 0) return;
     const int b = uniform(f.sequence), unit = uniform(f.place), tile = unit / a.kv_heads, head = unit % a.kv_heads;
-    const Shape shape = shape_of<ROWS>(a, b);
-    const int parts = uniform((shape.pages + most - 1) / most);
+    const int parts = uniform(shares.cuts(shares.at(b)));
     const Span span = new_tokens(a.seq, b);
-    const int row = blockIdx.x, at = tile * ROWS + row;
-    if (at >= uniform(span.n) * a.group) return;
-    // parts of the cut units before this sequence's
-    int before = 0;
-    for (int b0 = 0; b0 < b; b0 += 64) {
-        const int i = b0 + lane_id();
-        const Shape s = i < b ? shape_of<ROWS>(a, i) : Shape{0, 0};
-        before += s.pages > most ? (s.pages + most - 1) / most * s.tiles * a.kv_heads : 0;
-    }
-#pragma unroll
-    for (int off = 32; off; off >>= 1) before += __shfl_xor(before, off);
-    const int slot = uniform(before) + unit * parts;
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
-    const float *const from = a.parts + ((int64_t)slot * ROWS + row) * D + lane * E;
-    const float *const stat = a.parts + (int64_t)2 * PARTS * ROWS * D + ((int64_t)slot * ROWS + row) * 2;
-    float x[E] = {}, top = NONE, weight = 0.0f;
-#pragma unroll 8
-    for (int p = wave; p < parts; p += WAVES) {
-        const float mp = stat[(int64_t)p * ROWS * 2], lp = stat[(int64_t)p * ROWS * 2 + 1];
-        const float grown = fmaxf(top, mp);
-        const float old = top == NONE ? 1.0f : __builtin_amdgcn_exp2f(top - grown), by = mp == NONE ? 1.0f : __builtin_amdgcn_exp2f(mp - grown);
-        weight = weight * old + lp * by;
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = x[e] * old + from[(int64_t)p * ROWS * D + e] * by;
-        top = grown;
+    const int row = waves_a_row == 1 ? blockIdx.x * WAVES + wave : blockIdx.x, first = waves_a_row == 1 ? 0 : wave;
+    const int at = tile * ROWS + row;
+    const bool live = row < ROWS && at < uniform(span.n) * a.group;
+    if (!live && waves_a_row == 1) return;
+    // parts of the cut units before this one's
+    double before = 0.0;
+    for (int b0 = 0; b0 < b; b0 += 64) {
+        const Shape s = shares.shape(b0 + lane);
+        before += b0 + lane < b && cut(s) ? shares.cuts(s) * s.tiles * a.kv_heads : 0;
     }
+    const int slot = uniform((int)wave_sum(before)) + unit * parts;
+    const float *const from = a.parts + ((int64_t)slot * ROWS + min(row, ROWS - 1)) * D + lane * E;
+    const float *const stat = a.parts + (int64_t)2 * PARTS * ROWS * D + ((int64_t)slot * ROWS + min(row, ROWS - 1)) * 2;
+    float x[E] = {}, top = NONE, weight = 0.0f;
+    // 64 parts at a time: a lane has the maximum and the weight of one; then their sums, whose loads wait for nothing
+    for (int p0 = first; live && p0 < parts; p0 += 64 * waves_a_row) {
+        const int p = p0 + lane * waves_a_row;
+        const float2 own = p < parts ? *(const float2 *)(stat + (int64_t)p * ROWS * 2) : float2{NONE, 0.0f};
+        const float grown = fmaxf(top, column_max(row_max(own.x)));
+        const float old = top == NONE ? 1.0f : __builtin_amdgcn_exp2f(top - grown), by = own.x == NONE ? 1.0f : __builtin_amdgcn_exp2f(own.x - grown);
+        weight = weight * old + (float)wave_sum((double)(own.y * by));
+        top = grown;
+        const int n = min((parts - p0 + waves_a_row - 1) / waves_a_row, 64);
 #pragma unroll
-    for (int e = 0; e < E; ++e) sums[wave][lane * E + e] = x[e];
-    if (lane == 0) stats[wave][0] = top, stats[wave][1] = weight;
-    __syncthreads();
-    if (threadIdx.x >= D) return;
-    float t = NONE, w = 0.0f, y = 0.0f;
-    for (int i = 0; i < WAVES; ++i) t = fmaxf(t, stats[i][0]);
-    for (int i = 0; i < WAVES; ++i) {
-        const float by = stats[i][0] == NONE ? 1.0f : __builtin_amdgcn_exp2f(stats[i][0] - t);
-        w += by * stats[i][1], y += by * sums[i][threadIdx.x];
+        for (int e = 0; e < E; ++e) x[e] *= old;
+        for (int i0 = 0; i0 < n; i0 += 8)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int part = min(i0 + i, n - 1);
+                const float w = i0 + i < n ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), part)) : 0.0f;
+                const float *const y = from + (int64_t)(p0 + part * waves_a_row) * ROWS * D;
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[e] += w * y[e];
+            }
+    }
+    if (waves_a_row > 1) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) sums[wave][lane * E + e] = x[e];
+        if (lane == 0) stats[wave][0] = top, stats[wave][1] = weight;
+        __syncthreads();
+        if (wave > 0 || !live) return;
+        for (int i = 0; i < WAVES; ++i) top = fmaxf(top, stats[i][0]);
+        weight = 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = 0.0f;
+        for (int i = 0; i < WAVES; ++i) {
+            const float by = stats[i][0] == NONE ? 1.0f : __builtin_amdgcn_exp2f(stats[i][0] - top);
+            weight += by * stats[i][1];
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] += by * sums[i][lane * E + e];
+        }
     }
     const int token = uniform(span.begin) + at / a.group, h = head * a.group + at % a.group;
-    a.out[((int64_t)token * a.heads + h) * D + threadIdx.x] = bf16_rne(w == 0.0f ? 0.0f : y / w);
+    uint16_t *const to = a.out + ((int64_t)token * a.heads + h) * D + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) to[e] = bf16_rne(weight == 0.0f ? 0.0f : x[e] / weight);
 }
 
 // Rows of a tile: 16, or 32 where the sequences have more on average
@@ -459,11 +505,13 @@ hipError_t launch_cached_attention(Heads q, const Sequences &s, int heads, int k
     else
         tiles == 1 ? cached_attention_kernel<64, 1><<<blocks, threads, 0, stream>>>(a) : cached_attention_kernel<64, 2><<<blocks, threads, 0, stream>>>(a);
     if (cut) {
-        const dim3 joins((unsigned)rows, (unsigned)(units < PARTS ? units : PARTS));
+        const int most = units < PARTS ? (int)units : PARTS, used = s.cu || group > rows ? rows : group;
+        const int waves_a_row = (int64_t)most * used <= 4096 ? WAVES : 1;
+        const dim3 joins((unsigned)(waves_a_row == 1 ? (used + WAVES - 1) / WAVES : used), (unsigned)most);
         if (head_dim == 128)
-            tiles == 1 ? join_parts_kernel<128, 1><<<joins, threads, 0, stream>>>(a) : join_parts_kernel<128, 2><<<joins, threads, 0, stream>>>(a);
+            tiles == 1 ? join_parts_kernel<128, 1><<<joins, threads, 0, stream>>>(a, waves_a_row) : join_parts_kernel<128, 2><<<joins, threads, 0, stream>>>(a, waves_a_row);
         else
-            tiles == 1 ? join_parts_kernel<64, 1><<<joins, threads, 0, stream>>>(a) : join_parts_kernel<64, 2><<<joins, threads, 0, stream>>>(a);
+            tiles == 1 ? join_parts_kernel<64, 1><<<joins, threads, 0, stream>>>(a, waves_a_row) : join_parts_kernel<64, 2><<<joins, threads, 0, stream>>>(a, waves_a_row);
     }
     return hipGetLastError();
 }
