@@ -22,8 +22,9 @@ namespace fptq {
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 
-constexpr int WAVES = 4;                       // of a workgroup; they take every fourth page
-constexpr int MIN_SHARE = 16;                  // pages of a part at least
+constexpr int WAVES = 8;                       // of a workgroup; they take every eighth page
+constexpr int MIN_SHARE = 32;                  // pages of a part at least
+constexpr int MAX_GRID = 1024;
 constexpr int PARTS = 2048;                    // what all pages are shared out to, about
 
 struct DecodeArgs {
@@ -47,14 +48,15 @@ __device__ inline Shape shape_of(const DecodeArgs &a, int b)
     return {(rows + ROWS - 1) / ROWS, (int)min((int64_t)(length_of(a.seq, b) + PAGE - 1) / PAGE, a.seq.table_width)};
 }
 
-// How the pages are shared out: units of more than `most` pages, an even share of all and at least MIN_SHARE, are cut into equal parts.  Every wave
-// finds this out for itself, 64 sequences at a time; the shapes of the first 64 stay in its lanes.
+// How the pages are shared out: units of more than twice `most` pages, an even share of all and at least MIN_SHARE, are cut into equal parts of at most that.
+// (Cutting those of up to twice as many costs the join's 5 us and balances little.)  Every wave finds this out for itself, 64 sequences at a time; the
+// shapes of the first 64 stay in its lanes.
 template <int ROWS>
 struct Shares {
     const DecodeArgs &a;
     Shape first;
     int most;
-    __device__ explicit Shares(const DecodeArgs &args) : a(args), first(shape_of<ROWS>(args, lane_id())), most(1 << 30)
+    __device__ explicit Shares(const DecodeArgs &args) : a(args), first(shape_of<ROWS>(args, lane_id())), most(1 << 29)
     {
         if (!a.parts) return;
         double all = (double)first.tiles * first.pages;        // exact: below 2^53
@@ -63,7 +65,7 @@ struct Shares {
             all += (double)s.tiles * s.pages;
         }
         all = wave_sum(all) * a.kv_heads;
-        most = uniform((int)fmin(fmax(ceil(all * (1.0 / PARTS)), (double)MIN_SHARE), 0x1p30));
+        most = uniform((int)fmin(fmax(ceil(all * (1.0 / PARTS)), (double)MIN_SHARE), 0x1p29));
     }
     __device__ Shape shape(int b) const { return b < 64 ? first : shape_of<ROWS>(a, b); }      // of sequence b, a lane's own in its group of 64
     __device__ Shape at(int b) const                                                           // of any, for all lanes
@@ -71,7 +73,7 @@ struct Shares {
         if (b >= 64) return shape_of<ROWS>(a, b);
         return {__builtin_amdgcn_readlane(first.tiles, b), __builtin_amdgcn_readlane(first.pages, b)};
     }
-    __device__ int cuts(const Shape &s) const { return (s.pages + most - 1) / most; }
+    __device__ int cuts(const Shape &s) const { return s.pages > 2 * most ? (s.pages + most - 1) / most : 1; }
 };
 
 struct Unit {
@@ -102,7 +104,7 @@ __device__ inline bool find_unit(const DecodeArgs &a, int item, Unit &u)
         });
     if (f.sequence < 0) return false;
     const int b = uniform(f.sequence), place = uniform(f.place);
-    u.parts = uniform(max(shares.cuts(shares.at(b)), 1));
+    u.parts = uniform(shares.cuts(shares.at(b)));
     const int unit = place / u.parts;
     u.sequence = b, u.part = place % u.parts, u.tile = unit / a.kv_heads, u.head = unit % a.kv_heads;
     return true;
@@ -161,9 +163,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cached_attention_kernel(const D
     constexpr int ROWS = 16 * RT, KB = D / 64, DG = D / 16, PITCH = D + 4;
     __shared__ __attribute__((aligned(16))) float sums[WAVES][ROWS][PITCH];
     __shared__ float stats[WAVES][ROWS][2];
+    // The grid is for the most parts there can be, up to MAX_GRID; how many there are, and which, is known here only.
+    for (int item = blockIdx.x;; item += gridDim.x) {
     Unit u;
-    if (!find_unit<ROWS>(a, blockIdx.x, u)) return;
-    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
+    if (!find_unit<ROWS>(a, item, u)) return;
+    if (item != (int)blockIdx.x) __syncthreads();             // LDS is free again
+    int thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));             // what follows from it is not kept from part to part: there are no registers for that
+    const int lane = thread & 63, wave = uniform(thread >> 6), col = lane & 15, g = lane >> 4;
     const Span span = new_tokens(a.seq, u.sequence);
     const int begin = uniform(span.begin), n = uniform(span.n), length = uniform(length_of(a.seq, u.sequence));
     const int pages = (int)min((int64_t)(length + PAGE - 1) / PAGE, a.seq.table_width);
@@ -195,7 +202,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cached_attention_kernel(const D
     const int all_see = row0 + ROWS <= rows ? max(length - n + 1 + first_token, 0) : 0;      // keys below it need no mask
     const int some_see = max(length - n + 1 + last_token, 0);                                // keys from it on nobody sees
 
-    // this part's pages that anybody sees, every fourth one this wave's
+    // this part's pages that anybody sees, this wave's among them
     const int per = (pages + u.parts - 1) / u.parts, from = u.part * per;
     const int to = min(min(from + per, pages), (some_see + PAGE - 1) / PAGE);
     const int mine = max((to - from - wave + WAVES - 1) / WAVES, 0);
@@ -361,7 +368,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cached_attention_kernel(const D
     }
     __syncthreads();
     constexpr int PER_ROW = D / 8;
-    for (int at = threadIdx.x; at < ROWS * PER_ROW; at += 64 * WAVES) {
+    for (int at = thread; at < ROWS * PER_ROW; at += 64 * WAVES) {
         const int row = at / PER_ROW, d0 = at % PER_ROW * 8;
         if (row0 + row >= rows) continue;
         float top = NONE, weight = 0.0f;
@@ -387,16 +394,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cached_attention_kernel(const D
                 v4u{pack_bf16(x[0] * r, x[1] * r), pack_bf16(x[2] * r, x[3] * r), pack_bf16(y[0] * r, y[1] * r), pack_bf16(y[2] * r, y[3] * r)};
         }
     }
+    if (D == 128 && RT == 2) return;             // no registers to go on with: its grid has a workgroup for every part
+    }
 }
 
-// Joins the parts of a unit that was cut, a row to a wave, or to the four waves of a workgroup, which then take every fourth part.  blockIdx.y: the unit.
+// Joins the parts of a unit that was cut, a row to a wave, or to the waves of a workgroup, which then take every eighth part.  blockIdx.y: the unit.
 template <int D, int RT>
 __global__ __launch_bounds__(64 * WAVES) void join_parts_kernel(const DecodeArgs a, int waves_a_row)
 {
     constexpr int ROWS = 16 * RT, E = D / 64;
     __shared__ float sums[WAVES][D], stats[WAVES][2];
     const Shares<ROWS> shares(a);
-    const auto cut = [&](const Shape &s) { return s.pages > shares.most; };
+    const auto cut = [&](const Shape &s) { return shares.cuts(s) > 1; };
     const Found f = find_sequence(a.seq.count, blockIdx.y, [&](int b) {
         const Shape s = shares.shape(b);
         return cut(s) ? s.tiles * a.kv_heads : 0;
@@ -473,9 +482,9 @@ static int64_t most_units(int64_t tokens, int64_t sequences, int group, int kv_h
     const int64_t tiles = tokens * group / rows + sequences;        // of n rows: n / rows + 1 at most
     return (tiles < tokens * group ? tiles : tokens * group) * kv_heads;
 }
-static int64_t most_cut(int64_t units, int64_t table_width)         // parts of cut units: each longer than MIN_SHARE, and than an even share
+static int64_t most_cut(int64_t units, int64_t table_width)         // parts of cut units: MIN_SHARE pages at most, or an even share
 {
-    if (table_width <= MIN_SHARE) return 0;
+    if (table_width <= 2 * MIN_SHARE) return 0;
     const int64_t by_width = units * ((table_width + MIN_SHARE - 1) / MIN_SHARE);
     return by_width < 2 * PARTS ? by_width : 2 * PARTS;
 }
@@ -497,8 +506,8 @@ hipError_t launch_cached_attention(Heads q, const Sequences &s, int heads, int k
     const int64_t need = cached_attention_scratch_bytes(s.tokens, s.count, heads, kv_heads, head_dim, s.table_width);
     const bool cut = need > 0 && scratch && scratch_bytes >= need;
     DecodeArgs a = {q, s, cache, out, cut ? (float *)scratch : nullptr, heads, kv_heads, group, scale * 1.44269504088896341f};
-    const int64_t grid = units + (cut ? most_cut(units, s.table_width) : 0);
-    if (grid > 1 << 23) return hipErrorInvalidConfiguration;
+    const int64_t items = units + (cut ? most_cut(units, s.table_width) : 0), grid = items < MAX_GRID || (head_dim == 128 && tiles == 2) ? items : MAX_GRID;
+    if (items > 1 << 23) return hipErrorInvalidConfiguration;
     const dim3 threads(64 * WAVES), blocks((unsigned)grid);
     if (head_dim == 128)
         tiles == 1 ? cached_attention_kernel<128, 1><<<blocks, threads, 0, stream>>>(a) : cached_attention_kernel<128, 2><<<blocks, threads, 0, stream>>>(a);

@@ -70,10 +70,10 @@ def test_several_tokens_each(new, lengths, H, J, D):
     run(new, lengths, H, J, D, seed=H + sum(new))
 
 
-@pytest.mark.parametrize("H,J,D,new,lengths", [(4, 1, 64, [1], [2500]), (8, 2, 128, [1, 1, 1], [1100, 40, 1700]), (4, 1, 64, [6, 2], [1025, 3000]),
-                                               (16, 1, 128, [5, 1, 0], [1500, 1025, 90])])
+@pytest.mark.parametrize("H,J,D,new,lengths", [(4, 1, 64, [1], [5000]), (8, 2, 128, [1, 1, 1], [4200, 40, 6000]), (4, 1, 64, [6, 2], [4097, 9000]),
+                                               (16, 1, 128, [5, 1, 0], [4500, 5000, 90])])
 def test_long_sequences_shared_out_and_not(H, J, D, new, lengths):
-    """More than 16 pages are cut into parts.  Without scratch they are not; both are within the bound, and the parts' own order is the same every time."""
+    """More than 64 pages are cut into parts.  Without scratch they are not; both are within the bound, and the parts' own order is the same every time."""
     run(new, lengths, H, J, D, seed=1)
     g = torch.Generator(device="cuda").manual_seed(1)
     q, _, _ = projection(g, sum(new), H, J, D)
@@ -93,8 +93,21 @@ def test_long_sequences_shared_out_and_not(H, J, D, new, lengths):
 def test_very_many_short_and_long_sequences():
     rng = np.random.default_rng(3)
     lengths = [int(n) for n in rng.integers(1, 200, 150)]
-    lengths[70], lengths[149] = 2000, 1500
+    lengths[70], lengths[149] = 4500, 4700
     run([1] * 150, lengths, 4, 2, 64, seed=3, with_cu=False)
+
+
+@pytest.mark.parametrize("H,J,D,tokens", [(8, 8, 64, 1), (16, 1, 128, 2)])
+def test_a_wide_table_of_short_sequences(H, J, D, tokens):
+    """Room for many more parts than there are."""
+    lengths, new = [100, 70, 1, 4100] * 4, [tokens] * 16
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, _, _ = projection(g, sum(new), H, J, D)
+    table, codes, scales = filled(lengths, J, D, 3)
+    wide = np.full((16, 5000), -1, np.int32)
+    wide[:, :table.shape[1]] = table
+    out = fptq.fptq_cached_attention(q, cache_of(codes, scales), device(wide), device(lengths), device(starts(new)) if tokens > 1 else None)
+    check(out, *expected(q, new, lengths, table, codes, scales, D ** -0.5), D)
 
 
 def test_tokens_before_the_first_key_get_zeros():
@@ -164,7 +177,7 @@ def test_pages_past_32_bits():
 
 def test_replays_of_a_captured_call_follow_growing_lengths():
     J, D, H = 2, 128, 8
-    table, codes, scales = filled([1800, 700], J, D, 9, poison=False)
+    table, codes, scales = filled([4800, 700], J, D, 9, poison=False)
     cache = cache_of(codes, scales)
     q = torch.empty((2, H, D), dtype=torch.bfloat16, device="cuda")
     t, lengths, out = device(table), device([1, 1]), torch.empty((2, H, D), dtype=torch.bfloat16, device="cuda")
@@ -175,7 +188,7 @@ def test_replays_of_a_captured_call_follow_growing_lengths():
     with torch.cuda.graph(graph, stream=side):
         fptq.fptq_cached_attention(q, cache, t, lengths, out=out)
     g = torch.Generator(device="cuda").manual_seed(9)
-    for a, b in ((1, 700), (1025, 64), (1800, 0), (1799, 699)):
+    for a, b in ((1, 700), (4097, 64), (4800, 0), (4799, 699)):
         q.copy_(torch.randn(q.shape, device="cuda", generator=g).to(torch.bfloat16))
         lengths.copy_(device([a, b]))
         want = fptq.fptq_cached_attention(q, cache, t, lengths)
