@@ -22,10 +22,14 @@ namespace fptq {
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 
-constexpr int WAVES = 8;                       // of a workgroup; they take every eighth page
+// Waves of a workgroup, which take its pages in turn.  Eight share a unit's pages out further: 32 sequences of up to 4096 tokens, 16 rows, 36.9 us, with four waves
+// 41.1; 64 of up to 32768 475 and 507.  With 32 rows four are faster, each with more pages for what a wave costs at its beginning and end: 4 tokens behind
+// 131072 20.8 us, with eight 22.4.  (Loading two pages ahead instead of one: 21.5 and 23.9.)
+__host__ __device__ constexpr int waves_of(int row_tiles) { return row_tiles == 2 ? 4 : 8; }
+constexpr int JOIN_WAVES = 8;
 constexpr int MIN_SHARE = 32;                  // pages of a part at least
 constexpr int MAX_GRID = 1024;
-constexpr int PARTS = 2048;                    // what all pages are shared out to, about
+constexpr int PARTS = 1536;                    // what all pages are shared out to, about
 
 struct DecodeArgs {
     Heads q;
@@ -35,6 +39,7 @@ struct DecodeArgs {
     float *parts;                              // [2 PARTS][rows][D] sums, then [2 PARTS][rows][2] maxima and weights
     int heads, kv_heads, group;
     float scale;                               // times log2 e
+    int most_items;                            // parts and whole units there can be
 };
 
 struct Shape {
@@ -55,17 +60,24 @@ template <int ROWS>
 struct Shares {
     const DecodeArgs &a;
     Shape first;
-    int most;
-    __device__ explicit Shares(const DecodeArgs &args) : a(args), first(shape_of<ROWS>(args, lane_id())), most(1 << 29)
+    int most, items;                           // parts and whole units in all
+    __device__ explicit Shares(const DecodeArgs &args) : a(args), first{0, 0}, most(1 << 29)
     {
-        if (!a.parts) return;
-        double all = (double)first.tiles * first.pages;        // exact: below 2^53
-        for (int b0 = 64; b0 < a.seq.count; b0 += 64) {
-            const Shape s = shape_of<ROWS>(a, b0 + lane_id());
-            all += (double)s.tiles * s.pages;
+        if (!a.parts && !a.seq.cu) {           // as many units of every sequence, which it takes no lengths to know
+            items = a.most_items;
+            return;
         }
-        all = wave_sum(all) * a.kv_heads;
-        most = uniform((int)fmin(fmax(ceil(all * (1.0 / PARTS)), (double)MIN_SHARE), 0x1p29));
+        first = shape_of<ROWS>(a, lane_id());
+        if (a.parts) most = uniform((int)fmin(fmax(ceil(over_all([](const Shape &s) { return (double)s.tiles * s.pages; }) * (1.0 / PARTS)), (double)MIN_SHARE), 0x1p29));
+        items = uniform((int)fmin(over_all([&](const Shape &s) { return (double)s.tiles * cuts(s); }), (double)a.most_items));
+    }
+    // a sum over all kv heads of all sequences; exact, being below 2^53
+    template <class Of>
+    __device__ double over_all(Of of) const
+    {
+        double sum = of(first);
+        for (int b0 = 64; b0 < a.seq.count; b0 += 64) sum += of(shape_of<ROWS>(a, b0 + lane_id()));
+        return wave_sum(sum) * a.kv_heads;
     }
     __device__ Shape shape(int b) const { return b < 64 ? first : shape_of<ROWS>(a, b); }      // of sequence b, a lane's own in its group of 64
     __device__ Shape at(int b) const                                                           // of any, for all lanes
@@ -79,17 +91,14 @@ struct Shares {
 struct Unit {
     int sequence, head, tile, part, parts, slot;      // slot: where the part's results go
 };
-// Item `item` of the list of all parts: first those of units that are cut, then whole units
+// Item `item` of the list: first the parts of units that are cut, then whole units
 template <int ROWS>
-__device__ inline bool find_unit(const DecodeArgs &a, int item, Unit &u)
+__device__ inline Unit find_unit(const DecodeArgs &a, const Shares<ROWS> &shares, int item)
 {
-    u.slot = item;
-    if (!a.parts && !a.seq.cu) {                      // as many units of every sequence, which it takes no lengths to know
+    if (!a.parts && !a.seq.cu) {
         const int tiles = (a.group + ROWS - 1) / ROWS, unit = item % (tiles * a.kv_heads);
-        u.sequence = item / (tiles * a.kv_heads), u.tile = unit / a.kv_heads, u.head = unit % a.kv_heads, u.part = 0, u.parts = 1;
-        return u.sequence < a.seq.count;
+        return {item / (tiles * a.kv_heads), unit % a.kv_heads, unit / a.kv_heads, 0, 1, item};
     }
-    const Shares<ROWS> shares(a);
     Found f = {-1, item};
     if (a.parts)
         f = find_sequence(a.seq.count, item, [&](int b) {
@@ -102,12 +111,9 @@ __device__ inline bool find_unit(const DecodeArgs &a, int item, Unit &u)
             const Shape s = shares.shape(b);
             return shares.cuts(s) > 1 ? 0 : s.tiles * a.kv_heads;
         });
-    if (f.sequence < 0) return false;
-    const int b = uniform(f.sequence), place = uniform(f.place);
-    u.parts = uniform(shares.cuts(shares.at(b)));
-    const int unit = place / u.parts;
-    u.sequence = b, u.part = place % u.parts, u.tile = unit / a.kv_heads, u.head = unit % a.kv_heads;
-    return true;
+    const int b = uniform(max(f.sequence, 0)), place = uniform(f.place);
+    const int parts = uniform(shares.cuts(shares.at(b))), unit = place / parts;
+    return {b, unit % a.kv_heads, unit / a.kv_heads, place % parts, parts, item};
 }
 
 __device__ inline uint32_t widen(uint32_t codes, float scale, bool high)
@@ -158,15 +164,15 @@ __device__ inline float row_max(float v)
 constexpr float NONE = -__builtin_inff();
 
 template <int D, int RT>
-__global__ __launch_bounds__(64 * WAVES, 2) void cached_attention_kernel(const DecodeArgs a)
+__global__ __launch_bounds__(64 * waves_of(RT), 2) void cached_attention_kernel(const DecodeArgs a)
 {
-    constexpr int ROWS = 16 * RT, KB = D / 64, DG = D / 16, PITCH = D + 4;
+    constexpr int ROWS = 16 * RT, KB = D / 64, DG = D / 16, PITCH = D + 4, WAVES = waves_of(RT);
     __shared__ __attribute__((aligned(16))) float sums[WAVES][ROWS][PITCH];
     __shared__ float stats[WAVES][ROWS][2];
     // The grid is for the most parts there can be, up to MAX_GRID; how many there are, and which, is known here only.
-    for (int item = blockIdx.x;; item += gridDim.x) {
-    Unit u;
-    if (!find_unit<ROWS>(a, item, u)) return;
+    const Shares<ROWS> shares(a);
+    for (int item = blockIdx.x; item < shares.items; item += gridDim.x) {
+    const Unit u = find_unit<ROWS>(a, shares, item);
     if (item != (int)blockIdx.x) __syncthreads();             // LDS is free again
     int thread = threadIdx.x;
     asm volatile("" : "+v"(thread));             // what follows from it is not kept from part to part: there are no registers for that
@@ -231,16 +237,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cached_attention_kernel(const D
             ks = a.cache.ks[at], vs = a.cache.vs[at];
         }
         const int count = min(mine - i0, 64);
+        const auto base_of = [&](int i) { return ((int64_t)max(__builtin_amdgcn_readlane(id, i), 0) * a.kv_heads + u.head) * (PAGE * D); };
         v4u kc[KB][4], vc[DG];
-        auto base_of = [&](int i) { return ((int64_t)max(__builtin_amdgcn_readlane(id, i), 0) * a.kv_heads + u.head) * (PAGE * D); };
-        auto load_keys = [&](int i) {
+        const auto load_keys = [&](int i) {
             const uint8_t *const p = a.cache.k + base_of(i);
 #pragma unroll
             for (int k = 0; k < KB; ++k)
 #pragma unroll
                 for (int b = 0; b < 4; ++b) kc[k][b] = *(const v4u *)(p + k_lane + k * (PAGE * 64) + b * 256);
         };
-        auto load_values = [&](int i) {
+        const auto load_values = [&](int i) {
             const uint8_t *const p = a.cache.v + base_of(i);
 #pragma unroll
             for (int d = 0; d < DG; ++d) vc[d] = *(const v4u *)(p + v_lane + d * 256);
@@ -400,10 +406,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cached_attention_kernel(const D
 
 // Joins the parts of a unit that was cut, a row to a wave, or to the waves of a workgroup, which then take every eighth part.  blockIdx.y: the unit.
 template <int D, int RT>
-__global__ __launch_bounds__(64 * WAVES) void join_parts_kernel(const DecodeArgs a, int waves_a_row)
+__global__ __launch_bounds__(64 * JOIN_WAVES) void join_parts_kernel(const DecodeArgs a, int waves_a_row)
 {
     constexpr int ROWS = 16 * RT, E = D / 64;
-    __shared__ float sums[WAVES][D], stats[WAVES][2];
+    __shared__ float sums[JOIN_WAVES][D], stats[JOIN_WAVES][2];
     const Shares<ROWS> shares(a);
     const auto cut = [&](const Shape &s) { return shares.cuts(s) > 1; };
     const Found f = find_sequence(a.seq.count, blockIdx.y, [&](int b) {
@@ -415,7 +421,7 @@ __global__ __launch_bounds__(64 * WAVES) void join_parts_kernel(const DecodeArgs
     const int parts = uniform(shares.cuts(shares.at(b)));
     const Span span = new_tokens(a.seq, b);
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
-    const int row = waves_a_row == 1 ? blockIdx.x * WAVES + wave : blockIdx.x, first = waves_a_row == 1 ? 0 : wave;
+    const int row = waves_a_row == 1 ? blockIdx.x * JOIN_WAVES + wave : blockIdx.x, first = waves_a_row == 1 ? 0 : wave;
     const int at = tile * ROWS + row;
     const bool live = row < ROWS && at < uniform(span.n) * a.group;
     if (!live && waves_a_row == 1) return;
@@ -456,11 +462,11 @@ __global__ __launch_bounds__(64 * WAVES) void join_parts_kernel(const DecodeArgs
         if (lane == 0) stats[wave][0] = top, stats[wave][1] = weight;
         __syncthreads();
         if (wave > 0 || !live) return;
-        for (int i = 0; i < WAVES; ++i) top = fmaxf(top, stats[i][0]);
+        for (int i = 0; i < JOIN_WAVES; ++i) top = fmaxf(top, stats[i][0]);
         weight = 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] = 0.0f;
-        for (int i = 0; i < WAVES; ++i) {
+        for (int i = 0; i < JOIN_WAVES; ++i) {
             const float by = stats[i][0] == NONE ? 1.0f : __builtin_amdgcn_exp2f(stats[i][0] - top);
             weight += by * stats[i][1];
 #pragma unroll
@@ -505,22 +511,23 @@ hipError_t launch_cached_attention(Heads q, const Sequences &s, int heads, int k
     const int64_t units = most_units(s.tokens, s.count, group, kv_heads, rows);
     const int64_t need = cached_attention_scratch_bytes(s.tokens, s.count, heads, kv_heads, head_dim, s.table_width);
     const bool cut = need > 0 && scratch && scratch_bytes >= need;
-    DecodeArgs a = {q, s, cache, out, cut ? (float *)scratch : nullptr, heads, kv_heads, group, scale * 1.44269504088896341f};
+    DecodeArgs a = {q, s, cache, out, cut ? (float *)scratch : nullptr, heads, kv_heads, group, scale * 1.44269504088896341f, 0};
     const int64_t items = units + (cut ? most_cut(units, s.table_width) : 0), grid = items < MAX_GRID || (head_dim == 128 && tiles == 2) ? items : MAX_GRID;
     if (items > 1 << 23) return hipErrorInvalidConfiguration;
-    const dim3 threads(64 * WAVES), blocks((unsigned)grid);
+    a.most_items = (int)items;
+    const dim3 threads(64 * waves_of(tiles)), blocks((unsigned)grid);
     if (head_dim == 128)
         tiles == 1 ? cached_attention_kernel<128, 1><<<blocks, threads, 0, stream>>>(a) : cached_attention_kernel<128, 2><<<blocks, threads, 0, stream>>>(a);
     else
         tiles == 1 ? cached_attention_kernel<64, 1><<<blocks, threads, 0, stream>>>(a) : cached_attention_kernel<64, 2><<<blocks, threads, 0, stream>>>(a);
     if (cut) {
         const int most = units < PARTS ? (int)units : PARTS, used = s.cu || group > rows ? rows : group;
-        const int waves_a_row = (int64_t)most * used <= 4096 ? WAVES : 1;
-        const dim3 joins((unsigned)(waves_a_row == 1 ? (used + WAVES - 1) / WAVES : used), (unsigned)most);
+        const int waves_a_row = (int64_t)most * used <= 4096 ? JOIN_WAVES : 1;
+        const dim3 joins((unsigned)(waves_a_row == 1 ? (used + JOIN_WAVES - 1) / JOIN_WAVES : used), (unsigned)most);
         if (head_dim == 128)
-            tiles == 1 ? join_parts_kernel<128, 1><<<joins, threads, 0, stream>>>(a, waves_a_row) : join_parts_kernel<128, 2><<<joins, threads, 0, stream>>>(a, waves_a_row);
+            tiles == 1 ? join_parts_kernel<128, 1><<<joins, 64 * JOIN_WAVES, 0, stream>>>(a, waves_a_row) : join_parts_kernel<128, 2><<<joins, 64 * JOIN_WAVES, 0, stream>>>(a, waves_a_row);
         else
-            tiles == 1 ? join_parts_kernel<64, 1><<<joins, threads, 0, stream>>>(a, waves_a_row) : join_parts_kernel<64, 2><<<joins, threads, 0, stream>>>(a, waves_a_row);
+            tiles == 1 ? join_parts_kernel<64, 1><<<joins, 64 * JOIN_WAVES, 0, stream>>>(a, waves_a_row) : join_parts_kernel<64, 2><<<joins, 64 * JOIN_WAVES, 0, stream>>>(a, waves_a_row);
     }
     return hipGetLastError();
 }
