@@ -28,6 +28,7 @@ struct PromptArgs {
 };
 
 constexpr float NONE = -__builtin_inff();
+constexpr int QK_AHEAD = 4, PV_AHEAD = 4;
 constexpr int QT = 128, KTILE = 64;            // tokens of a workgroup, keys of a tile
 
 __device__ inline float other_half_max(float v)
@@ -55,8 +56,20 @@ __device__ inline uint2 read_column(const uint8_t *p)
     return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(p)));
 }
 
-// 16 bytes a lane from memory to LDS, which is written in the order of the lanes
-__device__ inline void copy_to_lds(__amdgpu_buffer_rsrc_t r, uint8_t *to, uint32_t offset) { __builtin_amdgcn_raw_ptr_buffer_load_lds(r, LDS_PTR(to), 16, offset, 0, 0, 0); }
+// 16 bytes a lane from memory to LDS, which is written in the order of the lanes, from `to` on.  As assembly, because the compiler, which cannot tell tiles apart,
+// would wait for the tile on its way before it reads the one that is there, every time (8192 tokens, 64 heads: 1096 us); it has no outputs, and what it
+// writes is waited for at the barrier, by s_waitcnt vmcnt(0).
+__device__ inline void copy_to_lds(v4i descriptor, uint32_t to, uint32_t offset)
+{
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(to), "v"(offset), "s"(descriptor) : "memory");
+}
+// raw buffer descriptor; reads past its end are zeros
+__device__ inline v4i descriptor_of(const void *base, int bytes)
+{
+    const uint64_t p = (uint64_t)base;
+    return v4i{uniform((int)p), uniform((int)(p >> 32) & 0xffff), uniform(bytes), RSRC_FLAGS};
+}
+__device__ inline uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)LDS_PTR((void *)p); }
 
 // bf16 pairs that hold an infinity or a NaN, as 0xffff each
 __device__ inline uint32_t not_finite(uint32_t w)
@@ -65,8 +78,8 @@ __device__ inline uint32_t not_finite(uint32_t w)
     return lo | hi;
 }
 
-// Blocks of QT tokens by the work in them, the most first: of every sequence long enough its block at one place, then the blocks one place before.
-// Workgroups begin in this order, so the last to end are short (nine prompts of 6000 tokens together: in the sequences' own order 99 us, so 78).
+// Blocks of QT tokens, those of the longest sequence first and a sequence's last block first: what ends last is short, and blocks that read the same keys and
+// values run at about the same time (the longest blocks of all sequences first, the next ones then: each reads them from memory again).
 struct Block {
     int sequence, place;
 };
@@ -78,23 +91,26 @@ __device__ inline Block find_block(const Sequences &s, int item)
         const int place = __builtin_amdgcn_readlane(first, 0) - 1 - item;
         return {place < 0 ? -1 : 0, place};
     }
-    // a sum over the sequences
-    const auto over_all = [&](auto of) {
-        int sum = of(first);
-        for (int b0 = 64; b0 < s.count; b0 += 64) sum += of(blocks_of(s, b0 + lane_id()));
+    // blocks of all sequences that have `least` of them or more
+    const auto blocks = [&](int least) {
+        int sum = first >= least ? first : 0;
+        for (int b0 = 64; b0 < s.count; b0 += 64) {
+            const int n = blocks_of(s, b0 + lane_id());
+            sum += n >= least ? n : 0;
+        }
         return __builtin_amdgcn_readlane(wave_prefix(sum), 63);
     };
-    const auto from_on = [&](int place) { return over_all([=](int n) { return max(n - place, 0); }); };      // blocks at this place or behind it
-    if (item >= from_on(0)) return {-1, 0};
-    int place = 0, above = 1;                         // the last place that has item or fewer blocks behind it
-    while (item < from_on(above)) place = above, above *= 2;
-    while (above - place > 1) {
-        const int middle = (place + above) / 2;
-        if (item < from_on(middle)) place = middle;
+    if (item >= blocks(1)) return {-1, 0};
+    int length = 1, above = 2;                        // blocks of the item's sequence: the most that at least `item` + 1 are in sequences of
+    while (item < blocks(above)) length = above, above *= 2;
+    while (above - length > 1) {
+        const int middle = (length + above) / 2;
+        if (item < blocks(middle)) length = middle;
         else above = middle;
     }
-    const Found f = find_sequence(s.count, item - from_on(place + 1), [&](int b) { return (b < 64 ? first : blocks_of(s, b)) > place ? 1 : 0; });
-    return {f.sequence, place};
+    const int rest = item - blocks(length + 1);
+    const Found f = find_sequence(s.count, rest / length, [&](int b) { return (b < 64 ? first : blocks_of(s, b)) == length ? 1 : 0; });
+    return {f.sequence, length - 1 - rest % length};
 }
 
 template <int D>
@@ -131,117 +147,182 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptAr
         const int r = (wave * COPIES + c) * ROWS_PER_COPY + lane / GRANULES, g = lane % GRANULES;
         k_off[c] = r * (uint32_t)k_row + key_granule<D>(r, g) * 16, v_off[c] = r * (uint32_t)v_row + value_granule<D>(r, g) * 16;
     }
+    const uint32_t to = uniform(lds_address(lds) + wave * COPIES * 1024);
     // rows past the sequence's end are beyond the descriptor's and arrive as zeros
-    auto fill = [&](int tile, int stage) {
-        const int left = min(n - tile * KTILE, KTILE);
-        const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc((void *)(k_base + (int64_t)tile * KTILE * k_row), 0, (left - 1) * (int)k_row + ROW, RSRC_FLAGS);
-        const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc((void *)(v_base + (int64_t)tile * KTILE * v_row), 0, (left - 1) * (int)v_row + ROW, RSRC_FLAGS);
+    const auto fill_keys = [&](int tile, int stage) {
+        const v4i r = descriptor_of(k_base + (int64_t)tile * KTILE * k_row, (min(n - tile * KTILE, KTILE) - 1) * (int)k_row + ROW);
 #pragma unroll
-        for (int c = 0; c < COPIES; ++c) {
-            copy_to_lds(kr, &lds[stage][0][(wave * COPIES + c) * 1024], k_off[c]);
-            copy_to_lds(vr, &lds[stage][1][(wave * COPIES + c) * 1024], v_off[c]);
-        }
+        for (int c = 0; c < COPIES; ++c) copy_to_lds(r, to + stage * 2 * TILE + c * 1024, k_off[c]);
+    };
+    const auto fill_values = [&](int tile, int stage) {
+        const v4i r = descriptor_of(v_base + (int64_t)tile * KTILE * v_row, (min(n - tile * KTILE, KTILE) - 1) * (int)v_row + ROW);
+#pragma unroll
+        for (int c = 0; c < COPIES; ++c) copy_to_lds(r, to + stage * 2 * TILE + TILE + c * 1024, v_off[c]);
     };
 
+    // where the lane reads: of keys granule 2 k + half of row col; of values four tokens a read, 4 half + t / 4 of eight, values 32 d + 16 part + 4 (t % 4) ..,
+    // of which it gets its own of each token
+    const int t = lane & 15, part = lane >> 4 & 1;
+    uint32_t k_at[KS], v_at[DB];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) k_at[k] = col * ROW + key_granule<D>(col, 2 * k + half) * 16;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+        const int r = 4 * half + (t >> 2), v = 32 * d + 16 * part + 4 * (t & 3);
+        v_at[d] = r * ROW + value_granule<D>(r, v / 8) * 16 + v % 8 * 2;
+    }
+
     v16f o[DB] = {};
-    float m = NONE, base = 0.0f, l = 0.0f;
-    const int tiles = (min(row0 + QT, n) + KTILE - 1) / KTILE;
-    fill(0, 0);
-    for (int tile = 0; tile < tiles; ++tile) {
-        const int stage = tile & 1;
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-        __syncthreads();
-        if (tile + 1 < tiles) fill(tile + 1, stage ^ 1);
-        const int key0 = tile * KTILE;
-        if (key0 > first + 31) continue;                     // beyond all of the wave's rows
-        v16f s[2] = {};
-        const uint8_t *const keys = lds[stage][0], *const values = lds[stage][1];
+    float m = NONE, l = 0.0f;
+    // scores of the tile in `stage`
+    const auto scores = [&](int stage, v16f(&s)[2]) {
+        const uint8_t *const keys = lds[stage][0];
+        s[0] = v16f{}, s[1] = v16f{};
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                const int r = b * 32 + col;
-                const v4u x = *(const v4u *)(keys + r * ROW + key_granule<D>(r, 2 * k + half) * 16);
-                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, x), q[k], s[b], 0, 0, 0);
-            }
-        const bool diagonal = key0 + KTILE - 1 > first;
-        if (diagonal) {
+        for (int k = 0; k < KS; ++k)
 #pragma unroll
             for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (key0 + b * 32 + (e >> 2) * 8 + half * 4 + (e & 3) > row) s[b][e] = NONE;
-        }
+                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, *(const v4u *)(keys + k_at[k] + b * 32 * ROW)), q[k], s[b], 0, 0, 0);
+    };
+    const auto largest = [&](const v16f(&s)[2]) {
         float top = s[0][0];
 #pragma unroll
         for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e >> 4][e & 15]);
-        top *= a.scale;
+        return top * a.scale;
+    };
+    const auto raise = [&](float top) {
         if (__any(top > m + 8.0f)) {
             const float grown = fmaxf(m, other_half_max(top));
             const float by = m == NONE ? 0.0f : __builtin_amdgcn_exp2f(m - grown);
-            m = grown, base = grown == NONE ? 0.0f : grown;
+            m = grown;
             l *= by;
 #pragma unroll
             for (int d = 0; d < DB; ++d) o[d] *= by;
         }
+    };
+    // weights of 16 keys, as the products want them
+    const auto weights = [&](const v16f(&s)[2], v8bf(&p)[4]) {
+        const float base = m == NONE ? 0.0f : m;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k >> 1][8 * (k & 1) + 2 * e], a.scale, -base));
+                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k >> 1][8 * (k & 1) + 2 * e + 1], a.scale, -base));
+                l += x + y;
+                w[e] = pack_bf16(x, y);
+            }
+            p[k] = __builtin_bit_cast(v8bf, v4u{w[0], w[1], w[2], w[3]});
+        }
+    };
+    const auto value_fragment = [&](int stage, int d, int k) {
+        const uint8_t *const from = lds[stage][1] + v_at[d] + k * 16 * ROW;
+        const uint2 x = read_column(from), y = read_column(from + 8 * ROW);
+        return v4u{x.x, x.y, y.x, y.y};
+    };
+
+    // A wave's last tile is the one with its own tokens, the only one with keys that some of its rows do not see.  Until then scores of a tile are made
+    // while the weights of the tile before are, and their maximum beside that tile's products: matrix instructions run under the others.
+    const int tiles = (min(row0 + QT, n) + KTILE - 1) / KTILE, own = min(tiles, first / KTILE + 1);
+    const auto turn = [&](int tile, int stage) {             // what all waves do before tile `tile`: its values and the next one's keys are there
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+        __syncthreads();
+        if (tile + 2 < tiles) fill_keys(tile + 2, stage);
+        if (tile + 1 < tiles) fill_values(tile + 1, stage ^ 1);
+    };
+    fill_keys(0, 0);
+    fill_values(0, 0);
+    if (tiles > 1) fill_keys(1, 1);
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    __syncthreads();
+    v16f s[2], later[2];
+    scores(0, s);
+    float top = largest(s);
+    const auto step = [&](int tile, int stage, const v16f(&now)[2], v16f(&next)[2]) {
+        turn(tile, stage);
+        raise(top);
+        __builtin_amdgcn_sched_barrier(0);
         v8bf p[4];
+        scores(stage ^ 1, next);
+        weights(now, p);
+        __builtin_amdgcn_sched_group_barrier(0x100, QK_AHEAD, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * KS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 112 / (2 * KS), 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, value_fragment(stage, d, k)), p[k], o[d], 0, 0, 0);
+        top = largest(next);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * PV_AHEAD, 0);
+#pragma unroll
+        for (int i = 0; i < 4 * DB; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 32 / (4 * DB), 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    int tile = 0;
+    for (; tile + 2 < own; tile += 2) {
+        step(tile, 0, s, later);
+        step(tile + 1, 1, later, s);
+    }
+    if (tile + 1 < own) {
+        step(tile, 0, s, later);
+        s[0] = later[0], s[1] = later[1];
+        ++tile;
+    }
+    {
+        const int stage = tile & 1, key0 = tile * KTILE;
+        turn(tile, stage);
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t w[4];
+            for (int e = 0; e < 16; ++e)
+                if (key0 + b * 32 + (e >> 2) * 8 + half * 4 + (e & 3) > row) s[b][e] = NONE;
+        raise(largest(s));
+        v8bf p[4];
+        weights(s, p);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * h + 2 * e], a.scale, -base));
-                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * h + 2 * e + 1], a.scale, -base));
-                    l += x + y;
-                    w[e] = pack_bf16(x, y);
-                }
-                p[2 * b + h] = __builtin_bit_cast(v8bf, v4u{w[0], w[1], w[2], w[3]});
-            }
-        const int t = lane & 15, part = lane >> 4 & 1;
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
+            for (int d = 0; d < DB; ++d) {
+                // An infinity or NaN that only some of the rows see would reach the others as 0 times itself.  It is taken out, and what it makes of the
+                // rows that see it is found by products of indicators: NaN counts as both infinities.
+                v4u w = value_fragment(stage, d, k), bad;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                // four tokens a read: 16 k + 8 j + 4 half + t / 4, values 32 d + 16 part + 4 (t % 4) ..; the lane gets its own value of each
-                uint2 x[2];
+                for (int e = 0; e < 4; ++e) bad[e] = not_finite(w[e]);
+                if (__any((bad[0] | bad[1] | bad[2] | bad[3]) != 0)) {
+                    v4u up, down, see;
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int r = 16 * k + 8 * j + 4 * half + (t >> 2), v = 32 * d + 16 * part + 4 * (t & 3);
-                    x[j] = read_column(values + r * ROW + value_granule<D>(r, v / 8) * 16 + v % 8 * 2);
-                }
-                v4u w = {x[0].x, x[0].y, x[1].x, x[1].y};
-                if (diagonal) {
-                    // An infinity or NaN that only some of the rows see would reach the others as 0 times itself.  It is taken out, and what it makes of the
-                    // rows that see it is found by products of indicators: NaN counts as both infinities.
-                    v4u bad;
+                    for (int e = 0; e < 4; ++e) {
+                        const int key = key0 + 16 * k + (e >> 1) * 8 + half * 4 + 2 * (e & 1);
+                        see[e] = (key <= row ? 0x3f80u : 0u) | (key + 1 <= row ? 0x3f800000u : 0u);
+                        const uint32_t negative = (w[e] & 0x8000u ? 0xffffu : 0u) | (w[e] & 0x80000000u ? 0xffff0000u : 0u);
+                        const uint32_t nan = (w[e] & 0x7fu ? 0xffffu : 0u) | (w[e] & 0x7f0000u ? 0xffff0000u : 0u);
+                        up[e] = bad[e] & (~negative | nan) & 0x3f803f80u, down[e] = bad[e] & (negative | nan) & 0x3f803f80u;
+                        w[e] &= ~bad[e];
+                    }
+                    const v16f zero = {};
+                    const v16f ups = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, up), __builtin_bit_cast(v8bf, see), zero, 0, 0, 0);
+                    const v16f downs = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, down), __builtin_bit_cast(v8bf, see), zero, 0, 0, 0);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) bad[e] = not_finite(w[e]);
-                    if (__any((bad[0] | bad[1] | bad[2] | bad[3]) != 0)) {
-                        v4u up, down, see;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int key = key0 + 16 * k + (e >> 1) * 8 + half * 4 + 2 * (e & 1);
-                            see[e] = (key <= row ? 0x3f80u : 0u) | (key + 1 <= row ? 0x3f800000u : 0u);
-                            const uint32_t negative = (w[e] & 0x8000u ? 0xffffu : 0u) | (w[e] & 0x80000000u ? 0xffff0000u : 0u);
-                            const uint32_t nan = (w[e] & 0x7fu ? 0xffffu : 0u) | (w[e] & 0x7f0000u ? 0xffff0000u : 0u);
-                            up[e] = bad[e] & (~negative | nan) & 0x3f803f80u, down[e] = bad[e] & (negative | nan) & 0x3f803f80u;
-                            w[e] &= ~bad[e];
-                        }
-                        const v16f zero = {};
-                        const v16f ups = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, up), __builtin_bit_cast(v8bf, see), zero, 0, 0, 0);
-                        const v16f downs = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, down), __builtin_bit_cast(v8bf, see), zero, 0, 0, 0);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            if (ups[e] > 0.0f) o[d][e] += __builtin_inff();
-                            if (downs[e] > 0.0f) o[d][e] -= __builtin_inff();
-                        }
+                    for (int e = 0; e < 16; ++e) {
+                        if (ups[e] > 0.0f) o[d][e] += __builtin_inff();
+                        if (downs[e] > 0.0f) o[d][e] -= __builtin_inff();
                     }
                 }
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, w), p[k], o[d], 0, 0, 0);
             }
     }
+    while (++tile < tiles) turn(tile, tile & 1);             // the waves of later tokens go on
     const float sum = other_half_sum(l), r = sum == 0.0f ? 0.0f : 1.0f / sum;
     if (row < n) {
         uint16_t *const to = a.out + ((int64_t)(begin + row) * a.heads + head) * D + half * 4;
