@@ -65,7 +65,8 @@ struct Found {
 template <class Count>
 __device__ inline Found find_sequence(int sequences, int item, Count count)
 {
-    const int lane = lane_id();
+    int lane = lane_id();
+    asm volatile("" : "+v"(lane));       // no address of it is kept over a caller's loops
     for (int b0 = 0; b0 < sequences; b0 += 64) {
         const int own = b0 + lane < sequences ? count(b0 + lane) : 0, upto = wave_prefix(own);
         const int all = __builtin_amdgcn_readlane(upto, 63);

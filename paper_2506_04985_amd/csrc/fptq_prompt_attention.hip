@@ -71,47 +71,53 @@ __device__ inline v4i descriptor_of(const void *base, int bytes)
 }
 __device__ inline uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)LDS_PTR((void *)p); }
 
-// bf16 pairs that hold an infinity or a NaN, as 0xffff each
+// bf16 pairs that hold an infinity or a NaN, as 0xffff each; whether a pair does, in bits 15 and 31
 __device__ inline uint32_t not_finite(uint32_t w)
 {
     const uint32_t lo = (w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
     return lo | hi;
 }
+__device__ inline uint32_t exponent_carry(uint32_t w) { return (w & 0x7f807f80u) + 0x00800080u; }
 
-// Blocks of QT tokens, those of the longest sequence first and a sequence's last block first: what ends last is short, and blocks that read the same keys and
-// values run at about the same time (the longest blocks of all sequences first, the next ones then: each reads them from memory again).
-struct Block {
-    int sequence, place;
+// What a workgroup does at a time: QT tokens of a head.  Items of the longest sequence come first and a sequence's last tokens first: what ends last is short,
+// and blocks that read the same keys and values run at about the same time (ordered by their own lengths each reads them from memory again).  More than
+// 64 sequences are taken in their own order.
+struct Item {
+    int begin, n, row0, head;                  // n 0: there is none
 };
-__device__ inline int blocks_of(const Sequences &s, int b) { return b < s.count ? (new_tokens(s, b).n + QT - 1) / QT : 0; }
-__device__ inline Block find_block(const Sequences &s, int item)
-{
-    const int first = blocks_of(s, lane_id());
-    if (s.count == 1) {
-        const int place = __builtin_amdgcn_readlane(first, 0) - 1 - item;
-        return {place < 0 ? -1 : 0, place};
+struct Items {
+    const PromptArgs &a;
+    int blocks, before;                        // of the lane's sequence, and those that come before them
+    __device__ explicit Items(const PromptArgs &args) : a(args), blocks(0), before(0)
+    {
+        const int lane = lane_id();
+        if (lane < a.seq.count) blocks = (new_tokens(a.seq, lane).n + QT - 1) / QT;
+        if (a.seq.count <= 64)
+            for (int j = 0; j < a.seq.count; ++j) {
+                const int other = __builtin_amdgcn_readlane(blocks, j);
+                before += other > blocks || (other == blocks && j < lane) ? other : 0;
+            }
     }
-    // blocks of all sequences that have `least` of them or more
-    const auto blocks = [&](int least) {
-        int sum = first >= least ? first : 0;
-        for (int b0 = 64; b0 < s.count; b0 += 64) {
-            const int n = blocks_of(s, b0 + lane_id());
-            sum += n >= least ? n : 0;
+    __device__ Item at(int index) const
+    {
+        const int block = index / a.heads, slot = index % a.heads;
+        Item i = {0, 0, 0, slot};
+        if (a.heads % 8 == 0) i.head = slot % 8 * (a.heads / 8) + slot / 8;      // an XCD, every eighth workgroup, gets heads that share keys and values
+        Found f;                                       // the place is from the sequence's last block on
+        if (a.seq.count <= 64) {
+            const uint64_t hit = __ballot(block >= before && block < before + blocks);
+            if (!hit) return i;
+            f.sequence = __builtin_ctzll(hit), f.place = block - __builtin_amdgcn_readlane(before, f.sequence);
+        } else {
+            f = find_sequence(a.seq.count, block, [&](int b) { return (new_tokens(a.seq, b).n + QT - 1) / QT; });
+            if (f.sequence < 0) return i;
         }
-        return __builtin_amdgcn_readlane(wave_prefix(sum), 63);
-    };
-    if (item >= blocks(1)) return {-1, 0};
-    int length = 1, above = 2;                        // blocks of the item's sequence: the most that at least `item` + 1 are in sequences of
-    while (item < blocks(above)) length = above, above *= 2;
-    while (above - length > 1) {
-        const int middle = (length + above) / 2;
-        if (item < blocks(middle)) length = middle;
-        else above = middle;
+        const Span span = new_tokens(a.seq, uniform(f.sequence));
+        i.begin = uniform(span.begin), i.n = uniform(span.n);
+        i.row0 = ((i.n + QT - 1) / QT - 1 - uniform(f.place)) * QT;
+        return i;
     }
-    const int rest = item - blocks(length + 1);
-    const Found f = find_sequence(s.count, rest / length, [&](int b) { return (b < 64 ? first : blocks_of(s, b)) == length ? 1 : 0; });
-    return {f.sequence, length - 1 - rest % length};
-}
+};
 
 template <int D>
 __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptArgs a)
@@ -121,14 +127,9 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptAr
     __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][TILE];         // [stage][keys, values]
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
 
-    // workgroups: heads within blocks of tokens; the XCDs (every eighth workgroup) get heads that share keys and values
-    const int block = blockIdx.x / a.heads, slot = blockIdx.x % a.heads;
-    const int head = a.heads % 8 == 0 ? slot % 8 * (a.heads / 8) + slot / 8 : slot;
-    const Block f = find_block(a.seq, block);
-    if (f.sequence < 0) return;
-    const Span span = new_tokens(a.seq, uniform(f.sequence));
-    const int begin = uniform(span.begin), n = uniform(span.n);
-    const int row0 = uniform(f.place) * QT;
+    const Item item = Items(a).at(blockIdx.x);
+    if (!item.n) return;
+    const int begin = item.begin, n = item.n, row0 = item.row0, head = item.head;
     const int first = row0 + wave * 32, row = first + col;
 
     v8bf q[KS];
@@ -222,6 +223,13 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptAr
         return v4u{x.x, x.y, y.x, y.y};
     };
 
+    const auto products = [&](int stage, const v8bf(&p)[4]) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int d = 0; d < DB; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, value_fragment(stage, d, k)), p[k], o[d], 0, 0, 0);
+    };
+
     // A wave's last tile is the one with its own tokens, the only one with keys that some of its rows do not see.  Until then scores of a tile are made
     // while the weights of the tile before are, and their maximum beside that tile's products: matrix instructions run under the others.
     const int tiles = (min(row0 + QT, n) + KTILE - 1) / KTILE, own = min(tiles, first / KTILE + 1);
@@ -254,11 +262,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptAr
             __builtin_amdgcn_sched_group_barrier(0x002, 112 / (2 * KS), 0);
         }
         __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int d = 0; d < DB; ++d)
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, value_fragment(stage, d, k)), p[k], o[d], 0, 0, 0);
+        products(stage, p);
         top = largest(next);
         __builtin_amdgcn_sched_group_barrier(0x100, 2 * PV_AHEAD, 0);
 #pragma unroll
@@ -282,6 +286,12 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptAr
     {
         const int stage = tile & 1, key0 = tile * KTILE;
         turn(tile, stage);
+        uint32_t carry = 0;                                   // of any value of the tile that is not finite
+#pragma unroll
+        for (int c = 0; c < TILE / 1024; ++c) {
+            const v4u w = *(const v4u *)(lds[stage][1] + c * 1024 + lane * 16);
+            carry |= exponent_carry(w[0]) | exponent_carry(w[1]) | exponent_carry(w[2]) | exponent_carry(w[3]);
+        }
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -290,25 +300,25 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptAr
         raise(largest(s));
         v8bf p[4];
         weights(s, p);
+        asm volatile("" : "+v"(l));                           // its terms are summed here and not kept until the end
+        if (!__any((carry & 0x80008000u) != 0)) {
+            products(stage, p);
+        } else {
+            // An infinity or NaN that only some of the rows see would reach the others as 0 times itself.  It is taken out, and what it makes of the
+            // rows that see it is found by products of indicators: NaN counts as both infinities.
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                // An infinity or NaN that only some of the rows see would reach the others as 0 times itself.  It is taken out, and what it makes of the
-                // rows that see it is found by products of indicators: NaN counts as both infinities.
-                v4u w = value_fragment(stage, d, k), bad;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) bad[e] = not_finite(w[e]);
-                if (__any((bad[0] | bad[1] | bad[2] | bad[3]) != 0)) {
-                    v4u up, down, see;
+                for (int d = 0; d < DB; ++d) {
+                    v4u w = value_fragment(stage, d, k), up, down, see;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int key = key0 + 16 * k + (e >> 1) * 8 + half * 4 + 2 * (e & 1);
                         see[e] = (key <= row ? 0x3f80u : 0u) | (key + 1 <= row ? 0x3f800000u : 0u);
-                        const uint32_t negative = (w[e] & 0x8000u ? 0xffffu : 0u) | (w[e] & 0x80000000u ? 0xffff0000u : 0u);
+                        const uint32_t bad = not_finite(w[e]), negative = (w[e] & 0x8000u ? 0xffffu : 0u) | (w[e] & 0x80000000u ? 0xffff0000u : 0u);
                         const uint32_t nan = (w[e] & 0x7fu ? 0xffffu : 0u) | (w[e] & 0x7f0000u ? 0xffff0000u : 0u);
-                        up[e] = bad[e] & (~negative | nan) & 0x3f803f80u, down[e] = bad[e] & (negative | nan) & 0x3f803f80u;
-                        w[e] &= ~bad[e];
+                        up[e] = bad & (~negative | nan) & 0x3f803f80u, down[e] = bad & (negative | nan) & 0x3f803f80u;
+                        w[e] &= ~bad;
                     }
                     const v16f zero = {};
                     const v16f ups = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, up), __builtin_bit_cast(v8bf, see), zero, 0, 0, 0);
@@ -318,20 +328,27 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptAr
                         if (ups[e] > 0.0f) o[d][e] += __builtin_inff();
                         if (downs[e] > 0.0f) o[d][e] -= __builtin_inff();
                     }
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, w), p[0], o[d], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, w), p[k], o[d], 0, 0, 0);
+                p[0] = p[1], p[1] = p[2], p[2] = p[3];
             }
+        }
     }
     while (++tile < tiles) turn(tile, tile & 1);             // the waves of later tokens go on
-    const float sum = other_half_sum(l), r = sum == 0.0f ? 0.0f : 1.0f / sum;
-    if (row < n) {
-        uint16_t *const to = a.out + ((int64_t)(begin + row) * a.heads + head) * D + half * 4;
+            // The lane holds values 8 i + 4 half .. of its row; halves exchange fours, so that each stores eight in a row.
+            const float sum = other_half_sum(l), r = sum == 0.0f ? 0.0f : 1.0f / sum;
+            uint16_t *const out = a.out + ((int64_t)(begin + row) * a.heads + head) * D + half * 8;
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
+            for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                *(uint2 *)(to + d * 32 + e * 8) = uint2{pack_bf16(o[d][4 * e] * r, o[d][4 * e + 1] * r), pack_bf16(o[d][4 * e + 2] * r, o[d][4 * e + 3] * r)};
-    }
+                for (int e = 0; e < 2; ++e) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = pack_bf16(o[d][8 * e + 2 * i] * r, o[d][8 * e + 2 * i + 1] * r);
+                    const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+                    if (row < n) *(v4u *)(out + d * 32 + e * 16) = v4u{x[0], y[0], x[1], y[1]};
+                }
 }
 
 hipError_t launch_prompt_attention(Heads q, Heads k, Heads v, const Sequences &s, int heads, int kv_heads, int head_dim, float scale, uint16_t *out,
