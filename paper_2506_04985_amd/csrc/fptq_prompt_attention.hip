@@ -79,24 +79,28 @@ __device__ inline uint32_t not_finite(uint32_t w)
 }
 __device__ inline uint32_t exponent_carry(uint32_t w) { return (w & 0x7f807f80u) + 0x00800080u; }
 
-// What a workgroup does at a time: QT tokens of a head.  Items of the longest sequence come first and a sequence's last tokens first: what ends last is short,
-// and blocks that read the same keys and values run at about the same time (ordered by their own lengths each reads them from memory again).  More than
-// 64 sequences are taken in their own order.
+// What a workgroup does: QT tokens of a head.  Items of the longest sequence come first and a sequence's last tokens first: what ends last is short, and
+// blocks that read the same keys and values run at about the same time (ordered by their own lengths each reads them from memory again).  More than
+// SORTED sequences are taken in their own order.
 struct Item {
     int begin, n, row0, head;                  // n 0: there is none
 };
 struct Items {
+    static constexpr int SORTED = 32;
     const PromptArgs &a;
     int blocks, before;                        // of the lane's sequence, and those that come before them
     __device__ explicit Items(const PromptArgs &args) : a(args), blocks(0), before(0)
     {
         const int lane = lane_id();
         if (lane < a.seq.count) blocks = (new_tokens(a.seq, lane).n + QT - 1) / QT;
-        if (a.seq.count <= 64)
-            for (int j = 0; j < a.seq.count; ++j) {
-                const int other = __builtin_amdgcn_readlane(blocks, j);
-                before += other > blocks || (other == blocks && j < lane) ? other : 0;
-            }
+        const int order = blocks * 64 + 63 - lane;       // of two with as many blocks the first one comes first; 2^17 blocks at most
+        if (a.seq.count <= SORTED)
+            for (int j0 = 0; j0 < a.seq.count; j0 += 8)  // eight at a time: one by one each waits for the one before, 180 cycles
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int other = __builtin_amdgcn_readlane(order, j0 + j);
+                    before += other > order ? other >> 6 : 0;
+                }
     }
     __device__ Item at(int index) const
     {
@@ -104,7 +108,7 @@ struct Items {
         Item i = {0, 0, 0, slot};
         if (a.heads % 8 == 0) i.head = slot % 8 * (a.heads / 8) + slot / 8;      // an XCD, every eighth workgroup, gets heads that share keys and values
         Found f;                                       // the place is from the sequence's last block on
-        if (a.seq.count <= 64) {
+        if (a.seq.count <= SORTED) {
             const uint64_t hit = __ballot(block >= before && block < before + blocks);
             if (!hit) return i;
             f.sequence = __builtin_ctzll(hit), f.place = block - __builtin_amdgcn_readlane(before, f.sequence);
@@ -117,6 +121,11 @@ struct Items {
         i.row0 = ((i.n + QT - 1) / QT - 1 - uniform(f.place)) * QT;
         return i;
     }
+};
+
+template <int N>
+struct Halves {
+    static constexpr int value = N;
 };
 
 template <int D>
@@ -173,6 +182,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptAr
         v_at[d] = r * ROW + value_granule<D>(r, v / 8) * 16 + v % 8 * 2;
     }
 
+    constexpr Halves<2> ALL;
     v16f o[DB] = {};
     float m = NONE, l = 0.0f;
     // scores of the tile in `stage`
@@ -185,10 +195,11 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptAr
             for (int b = 0; b < 2; ++b)
                 s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, *(const v4u *)(keys + k_at[k] + b * 32 * ROW)), q[k], s[b], 0, 0, 0);
     };
-    const auto largest = [&](const v16f(&s)[2]) {
+    // of the tile's first 32 keys, or of all
+    const auto largest = [&](auto halves, const v16f(&s)[2]) {
         float top = s[0][0];
 #pragma unroll
-        for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e >> 4][e & 15]);
+        for (int e = 1; e < 16 * halves.value; ++e) top = fmaxf(top, s[e >> 4][e & 15]);
         return top * a.scale;
     };
     const auto raise = [&](float top) {
@@ -201,11 +212,11 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptAr
             for (int d = 0; d < DB; ++d) o[d] *= by;
         }
     };
-    // weights of 16 keys, as the products want them
-    const auto weights = [&](const v16f(&s)[2], v8bf(&p)[4]) {
+    // weights of 16 keys each, as the products want them
+    const auto weights = [&](auto halves, const v16f(&s)[2], v8bf(&p)[4]) {
         const float base = m == NONE ? 0.0f : m;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < 2 * halves.value; ++k) {
             uint32_t w[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -223,9 +234,9 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptAr
         return v4u{x.x, x.y, y.x, y.y};
     };
 
-    const auto products = [&](int stage, const v8bf(&p)[4]) {
+    const auto products = [&](auto halves, int stage, const v8bf(&p)[4]) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 2 * halves.value; ++k)
 #pragma unroll
             for (int d = 0; d < DB; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, value_fragment(stage, d, k)), p[k], o[d], 0, 0, 0);
     };
@@ -244,16 +255,20 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptAr
     if (tiles > 1) fill_keys(1, 1);
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
     __syncthreads();
+    if (first >= n) {                                        // none of the wave's rows is there: it copies for the others
+        for (int tile = 0; tile < tiles; ++tile) turn(tile, tile & 1);
+        return;
+    }
     v16f s[2], later[2];
     scores(0, s);
-    float top = largest(s);
+    float top = largest(ALL, s);
     const auto step = [&](int tile, int stage, const v16f(&now)[2], v16f(&next)[2]) {
         turn(tile, stage);
         raise(top);
         __builtin_amdgcn_sched_barrier(0);
         v8bf p[4];
         scores(stage ^ 1, next);
-        weights(now, p);
+        weights(ALL, now, p);
         __builtin_amdgcn_sched_group_barrier(0x100, QK_AHEAD, 0);
 #pragma unroll
         for (int i = 0; i < 2 * KS; ++i) {
@@ -262,8 +277,8 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptAr
             __builtin_amdgcn_sched_group_barrier(0x002, 112 / (2 * KS), 0);
         }
         __builtin_amdgcn_sched_barrier(0);
-        products(stage, p);
-        top = largest(next);
+        products(ALL, stage, p);
+        top = largest(ALL, next);
         __builtin_amdgcn_sched_group_barrier(0x100, 2 * PV_AHEAD, 0);
 #pragma unroll
         for (int i = 0; i < 4 * DB; ++i) {
@@ -284,30 +299,34 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptAr
         ++tile;
     }
     {
-        const int stage = tile & 1, key0 = tile * KTILE;
+        const int stage = tile & 1, key0 = tile * KTILE, halves = (first / 32 & 1) + 1;
         turn(tile, stage);
-        uint32_t carry = 0;                                   // of any value of the tile that is not finite
+        // The wave's own 32 tokens are the last or the first half of the tile, and what is behind them nobody sees.
+        v8bf p[4];
+        uint32_t carry = 0;                                   // of any of their values that is not finite
+        const auto last = [&](auto halves) {
+            constexpr int own_half = halves.value - 1;
 #pragma unroll
-        for (int c = 0; c < TILE / 1024; ++c) {
-            const v4u w = *(const v4u *)(lds[stage][1] + c * 1024 + lane * 16);
-            carry |= exponent_carry(w[0]) | exponent_carry(w[1]) | exponent_carry(w[2]) | exponent_carry(w[3]);
-        }
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
+            for (int c = 0; c < TILE / 2048; ++c) {
+                const v4u w = *(const v4u *)(lds[stage][1] + own_half * (TILE / 2) + c * 1024 + lane * 16);
+                carry |= exponent_carry(w[0]) | exponent_carry(w[1]) | exponent_carry(w[2]) | exponent_carry(w[3]);
+            }
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-                if (key0 + b * 32 + (e >> 2) * 8 + half * 4 + (e & 3) > row) s[b][e] = NONE;
-        raise(largest(s));
-        v8bf p[4];
-        weights(s, p);
-        asm volatile("" : "+v"(l));                           // its terms are summed here and not kept until the end
-        if (!__any((carry & 0x80008000u) != 0)) {
-            products(stage, p);
-        } else {
+                if ((e >> 2) * 8 + half * 4 + (e & 3) > col) s[own_half][e] = NONE;
+            raise(largest(halves, s));
+            weights(halves, s, p);
+            asm volatile("" : "+v"(l));                       // its terms are summed here and not kept until the end
+            carry = __any((carry & 0x80008000u) != 0);
+            if (!carry) products(halves, stage, p);
+        };
+        if (halves == 2) last(Halves<2>());
+        else last(Halves<1>());
+        if (carry) {
             // An infinity or NaN that only some of the rows see would reach the others as 0 times itself.  It is taken out, and what it makes of the
             // rows that see it is found by products of indicators: NaN counts as both infinities.
 #pragma unroll 1
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < 2 * halves; ++k) {
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
                     v4u w = value_fragment(stage, d, k), up, down, see;
@@ -336,19 +355,19 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptAr
         }
     }
     while (++tile < tiles) turn(tile, tile & 1);             // the waves of later tokens go on
-            // The lane holds values 8 i + 4 half .. of its row; halves exchange fours, so that each stores eight in a row.
-            const float sum = other_half_sum(l), r = sum == 0.0f ? 0.0f : 1.0f / sum;
-            uint16_t *const out = a.out + ((int64_t)(begin + row) * a.heads + head) * D + half * 8;
+    // The lane holds values 8 i + 4 half .. of its row; halves exchange fours, so that each stores eight in a row.
+    const float sum = other_half_sum(l), r = sum == 0.0f ? 0.0f : 1.0f / sum;
+    uint16_t *const out = a.out + ((int64_t)(begin + row) * a.heads + head) * D + half * 8;
 #pragma unroll
-            for (int d = 0; d < DB; ++d)
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    uint32_t w[4];
+        for (int e = 0; e < 2; ++e) {
+            uint32_t w[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) w[i] = pack_bf16(o[d][8 * e + 2 * i] * r, o[d][8 * e + 2 * i + 1] * r);
-                    const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-                    if (row < n) *(v4u *)(out + d * 32 + e * 16) = v4u{x[0], y[0], x[1], y[1]};
-                }
+            for (int i = 0; i < 4; ++i) w[i] = pack_bf16(o[d][8 * e + 2 * i] * r, o[d][8 * e + 2 * i + 1] * r);
+            const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+            if (row < n) *(v4u *)(out + d * 32 + e * 16) = v4u{x[0], y[0], x[1], y[1]};
+        }
 }
 
 hipError_t launch_prompt_attention(Heads q, Heads k, Heads v, const Sequences &s, int heads, int kv_heads, int head_dim, float scale, uint16_t *out,
