@@ -10,7 +10,6 @@
 #include <cmath>
 #include <initializer_list>
 
-#include <ATen/EmptyTensor.h>
 #include <torch/extension.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -20,8 +19,6 @@ namespace {
 
 // torch._C functions: the device, the raw handle of its current stream, and whether that stream is being captured
 PyObject *g_device = nullptr, *g_stream = nullptr, *g_capturing = nullptr;
-
-thread_local long t_device = -1;       // the current device, as the call that this thread is making found it
 
 struct Slow {};        // thrown where the call is left to the Python wrapper
 
@@ -106,11 +103,7 @@ struct Output {
     void allocate()
     {
         if (dims == 0) return;
-        const at::IntArrayRef sizes(shape.data(), dims);
-        // on the current device straight from its allocator: at::empty's way there through the dispatcher takes 0.5 us of a call's 5.5
-        c10::Allocator *const allocator = device.is_cuda() && device.index() == t_device ? c10::GetAllocator(at::kCUDA) : nullptr;
-        made = allocator ? at::Tensor(at::detail::empty_generic(sizes, allocator, c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt))
-                         : at::empty(sizes, at::TensorOptions().dtype(type).device(device));
+        made = at::empty(at::IntArrayRef(shape.data(), dims), at::TensorOptions().dtype(type).device(device));
         ptr = made.data_ptr(), numel = made.numel();
     }
     PyObject *take()                 // a new reference to the tensor, None for no output
@@ -160,7 +153,6 @@ Where where()
     void *p = PyLong_AsVoidPtr(s);
     Py_DECREF(s);
     if (PyErr_Occurred()) throw Slow();
-    t_device = index;
     return {index, p};
 }
 
