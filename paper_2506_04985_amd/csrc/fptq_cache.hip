@@ -116,31 +116,68 @@ struct AppendArgs {
     int page_slots, query_parts;         // pages that the new tokens can touch; waves a token's query heads are spread over
 };
 
+// A sequence's new tokens and the position of the first of them (negative for a length that does not count them)
+struct Place {
+    int sequence, begin, n, at;
+};
+__device__ inline Place place_of(const Sequences &s, int b)
+{
+    const Span span = new_tokens(s, b);
+    return {b, span.begin, span.n, length_of(s, b) - span.n};
+}
+// The first sequence for which `is` holds, all lanes with one each; 64 a step.  sequence -1: none.
+template <class Is>
+__device__ inline Place first_of(const Sequences &s, Is is)
+{
+    const int lane = lane_id();
+    for (int b0 = 0; b0 < s.count; b0 += 64) {
+        const Place own = b0 + lane < s.count ? place_of(s, b0 + lane) : Place{-1, 0, 0, 0};
+        const uint64_t hit = __ballot(is(own));
+        if (hit) {
+            const int at = __builtin_ctzll(hit);
+            return {b0 + at, __builtin_amdgcn_readlane(own.begin, at), __builtin_amdgcn_readlane(own.n, at), __builtin_amdgcn_readlane(own.at, at)};
+        }
+    }
+    return {-1, 0, 0, 0};
+}
+
 // The new tokens of one page: rows first .. last - 1 of it, tokens from `token` on
 struct PageRows {
     int first, last, token, position;    // position: of row 0
-    int64_t page;                        // -1: the table names none
+    const int32_t *entry;                // of the table, NULL if it has none
 };
-__device__ inline bool page_rows(const AppendArgs &a, int slot, PageRows &r)
+__device__ inline bool page_rows(const Sequences &s, int slot, PageRows &r)
 {
-    const Sequences &s = a.seq;
-    Found f = {slot, 0};
-    if (s.cu)
-        f = find_sequence(s.count, slot, [&](int i) {
-            const int n = new_tokens(s, i).n, at = length_of(s, i) - n;
-            return n ? ((at + n - 1) >> 6) - (at >> 6) + 1 : 0;
+    Place p;
+    int before = 0;                      // pages that sequences before this one touch
+    if (s.cu) {
+        int all = 0;
+        p = first_of(s, [&](const Place &i) {
+            const int own = i.n > 0 ? ((i.at + i.n - 1) >> 6) - (i.at >> 6) + 1 : 0, upto = all + wave_prefix(own);
+            all = __builtin_amdgcn_readlane(upto, 63);
+            const uint64_t hit = __ballot(slot < upto);
+            if (hit) before = __builtin_amdgcn_readlane(upto - own, __builtin_ctzll(hit));
+            return slot < upto;
         });
-    const int b = uniform(f.sequence);
-    if (b < 0 || b >= s.count) return false;
-    const Span span = new_tokens(s, b);
-    const int n = uniform(span.n), begin = uniform(span.begin);
-    const int at = uniform(length_of(s, b)) - n, p = (at >> 6) + f.place;      // negative for a length that does not count the new tokens
-    r.position = p * PAGE;
-    r.first = max(at - r.position, 0), r.last = min(at + n - r.position, PAGE);
-    r.token = begin + r.position + r.first - at;
-    const int page = p >= 0 && p < s.table_width ? uniform(s.table[(int64_t)b * s.table_width + p]) : -1;
-    r.page = page >= 0 && page < a.cache.pages ? page : -1;
+    } else if (slot < s.count) {
+        p = place_of(s, slot);
+        p.at = uniform(p.at);
+    } else {
+        return false;
+    }
+    if (p.sequence < 0) return false;
+    const int page = (p.at >> 6) + slot * (s.cu ? 1 : 0) - before;
+    r.position = page * PAGE;
+    r.first = max(p.at - r.position, 0), r.last = min(p.at + p.n - r.position, PAGE);
+    r.token = p.begin + r.position + r.first - p.at;
+    r.entry = page >= 0 && page < s.table_width ? s.table + (int64_t)p.sequence * s.table_width + page : nullptr;
     return true;
+}
+// its number, -1 if the table names none of the cache
+__device__ inline int64_t page_number(const AppendArgs &a, const PageRows &r)
+{
+    const int page = r.entry ? uniform(*r.entry) : -1;
+    return page >= 0 && page < a.cache.pages ? page : -1;
 }
 
 // the largest magnitude over a workgroup of four waves
@@ -159,12 +196,23 @@ __device__ inline void append_keys(const AppendArgs &a, const PageRows &r, int j
     constexpr int U = D / 16, ROWS = 256 / U, PASSES = PAGE / ROWS;
     const int u = threadIdx.x % U, row0 = threadIdx.x / U;
     const Runs run = runs_of(u, a.rope_dims, INTERLEAVED);
-    uint8_t *const to = a.cache.k + (r.page * a.kv_heads + j) * (PAGE * D);
-    float *const scale_at = a.cache.ks + r.page * a.kv_heads + j;
+    // the rows first, which need no page
+    v4u lo[PASSES], hi[PASSES];
+    Angles angles[PASSES];
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+        const int row = min(max(row0 + p * ROWS, r.first), r.last - 1);
+        const uint16_t *const from = a.k.p + (int64_t)(r.token + row - r.first) * a.k.token + j * a.k.head;
+        lo[p] = *(const v4u *)(from + run.lo), hi[p] = *(const v4u *)(from + run.hi);
+        angles[p] = angles_of(a.rope, a.positions, a.rope_dims, r.position + row, u, run.rotated);
+    }
+    const int64_t page = page_number(a, r);
+    uint8_t *const to = a.cache.k + (page * a.kv_heads + j) * (PAGE * D);
+    float *const scale_at = a.cache.ks + page * a.kv_heads + j;
     constexpr int GRANULES = D / 64 * PAGE * 4 / 256;
     v4u old[GRANULES];
     float old_scale = 0.0f;
-    const bool older = r.page >= 0 && r.first > 0;
+    const bool older = page >= 0 && r.first > 0;
     if (older) {
         old_scale = *scale_at;
 #pragma unroll
@@ -175,21 +223,18 @@ __device__ inline void append_keys(const AppendArgs &a, const PageRows &r, int j
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
         const int row = row0 + p * ROWS;
+        rotate<INTERLEAVED>(x[p], lo[p], hi[p], angles[p], run.rotated);
         if (row >= r.first && row < r.last) {
-            const int64_t token = r.token + row - r.first;
-            const uint16_t *const from = a.k.p + token * a.k.token + j * a.k.head;
-            const v4u lo = *(const v4u *)(from + run.lo), hi = *(const v4u *)(from + run.hi);
-            rotate<INTERLEAVED>(x[p], lo, hi, angles_of(a.rope, a.positions, a.rope_dims, r.position + row, u, run.rotated), run.rotated);
 #pragma unroll
             for (int e = 0; e < 16; ++e) largest = max(largest, magnitude(x[p][e]));
             if (a.k_out) {
-                uint16_t *const out = a.k_out + (token * a.kv_heads + j) * D;
+                uint16_t *const out = a.k_out + ((int64_t)(r.token + row - r.first) * a.kv_heads + j) * D;
                 *(v4u *)(out + run.lo) = packed(x[p]), *(v4u *)(out + run.hi) = packed(x[p] + 8);
             }
         }
     }
     largest = workgroup_max(largest, lds);
-    if (r.page < 0) return;
+    if (page < 0) return;
     const float scale = fmaxf(__uint_as_float(scale_bits(largest)), old_scale), unit = reciprocal_of(__float_as_uint(scale));
     if (threadIdx.x == 0) *scale_at = scale;
     if (older && scale > old_scale) {
@@ -225,13 +270,23 @@ __device__ inline void append_values(const AppendArgs &a, const PageRows &r, int
 {
     constexpr int E = D / 64;
     const int lane = threadIdx.x & 63, t0 = threadIdx.x >> 6 << 4, d0 = lane * E;
-    uint8_t *const to = a.cache.v + (r.page * a.kv_heads + j) * (PAGE * D) + t0 * D + d0 * 16;
-    float *const scale_at = a.cache.vs + r.page * a.kv_heads + j;
     const int first = min(max(r.first - t0, 0), 16), last = min(max(r.last - t0, 0), 16);
     const bool whole = first == 0 && last == 16;
+    uint32_t w[16];                      // the rows first, which need no page
+#pragma unroll
+    for (int t = 0; t < 16; ++t) {
+        w[t] = 0;
+        if (t >= first && t < last) {
+            const uint16_t *const from = a.v.p + (int64_t)(r.token + t0 + t - r.first) * a.v.token + j * a.v.head + d0;
+            w[t] = E == 2 ? *(const uint32_t *)from : *from;
+        }
+    }
+    const int64_t page = page_number(a, r);
+    uint8_t *const to = a.cache.v + (page * a.kv_heads + j) * (PAGE * D) + t0 * D + d0 * 16;
+    float *const scale_at = a.cache.vs + page * a.kv_heads + j;
     v4u old[E];
     float old_scale = 0.0f;
-    if (r.page >= 0) {
+    if (page >= 0) {
         if (r.first > 0) old_scale = *scale_at;
         if (!whole) {
 #pragma unroll
@@ -242,18 +297,13 @@ __device__ inline void append_values(const AppendArgs &a, const PageRows &r, int
     uint32_t largest = 0;
 #pragma unroll
     for (int t = 0; t < 16; ++t) {
-        uint32_t w = 0;
-        if (t >= first && t < last) {
-            const uint16_t *const from = a.v.p + (int64_t)(r.token + t0 + t - r.first) * a.v.token + j * a.v.head + d0;
-            w = E == 2 ? *(const uint32_t *)from : *from;
-        }
-        x[0][t] = bf16_lo(w);
-        if (E == 2) x[E - 1][t] = bf16_hi(w);
+        x[0][t] = bf16_lo(w[t]);
+        if (E == 2) x[E - 1][t] = bf16_hi(w[t]);
 #pragma unroll
         for (int e = 0; e < E; ++e) largest = max(largest, magnitude(x[e][t]));
     }
     largest = workgroup_max(largest, lds);
-    if (r.page < 0) return;
+    if (page < 0) return;
     const float scale = fmaxf(__uint_as_float(scale_bits(largest)), old_scale), unit = reciprocal_of(__float_as_uint(scale));
     if (threadIdx.x == 0) *scale_at = scale;
     const bool raised = first > 0 && scale > old_scale;
@@ -286,19 +336,9 @@ __device__ inline void rotate_queries(const AppendArgs &a, int wave)
     const Sequences &s = a.seq;
     const int token = wave / a.query_parts, part = wave % a.query_parts;
     if (token >= s.tokens) return;
-    int b = token;
-    if (s.cu) {                                          // the last sequence that begins at or before the token
-        int lo = 0, hi = s.count - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (s.cu[mid] <= token) lo = mid;
-            else hi = mid - 1;
-        }
-        b = lo;
-    }
-    const auto [begin, n] = new_tokens(s, b);
-    if (token < begin || token >= begin + n) return;     // of no sequence
-    const int position = length_of(s, b) - n + token - begin;
+    const Place p = s.cu ? first_of(s, [=](const Place &i) { return token >= i.begin && token < i.begin + i.n; }) : place_of(s, token);
+    if (p.sequence < 0) return;                          // of no sequence
+    const int position = p.at + token - p.begin;
     const int lane = threadIdx.x & 63, u = lane % U;
     const Runs run = runs_of(u, a.rope_dims, INTERLEAVED);
     const Angles t = angles_of(a.rope, a.positions, a.rope_dims, position, u, run.rotated);
@@ -324,7 +364,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs a)
     }
     const int j = unit % a.kv_heads, slot = unit / a.kv_heads >> 1;
     PageRows r;
-    if (!page_rows(a, slot, r)) return;
+    if (!page_rows(a.seq, slot, r)) return;
     if (unit / a.kv_heads & 1) append_values<D>(a, r, j, lds);
     else append_keys<D, INTERLEAVED>(a, r, j, lds);
 }

@@ -164,8 +164,12 @@ __device__ inline float row_max(float v)
 constexpr float NONE = -__builtin_inff();
 
 template <int D, int RT>
-__global__ __launch_bounds__(64 * waves_of(RT), 2) void cached_attention_kernel(const DecodeArgs a)
+__global__ __launch_bounds__(64 * waves_of(RT), 2) void cached_attention_kernel(const int32_t *lengths, const int32_t *table_at, const int32_t *cu, const uint16_t *q_at, int64_t q_token,
+                                                                                  int64_t q_head, int32_t kv_heads, int32_t group, const DecodeArgs rest)
 {
+    // what a workgroup needs first comes with the dispatch
+    DecodeArgs a = rest;
+    a.seq.lengths = lengths, a.seq.table = table_at, a.seq.cu = cu, a.q = {q_at, q_token, q_head}, a.kv_heads = kv_heads, a.group = group;
     constexpr int ROWS = 16 * RT, KB = D / 64, DG = D / 16, PITCH = D + 4, WAVES = waves_of(RT);
     __shared__ __attribute__((aligned(16))) float sums[WAVES][ROWS][PITCH];
     __shared__ float stats[WAVES][ROWS][2];
@@ -516,10 +520,9 @@ hipError_t launch_cached_attention(Heads q, const Sequences &s, int heads, int k
     if (items > 1 << 23) return hipErrorInvalidConfiguration;
     a.most_items = (int)items;
     const dim3 threads(64 * waves_of(tiles)), blocks((unsigned)grid);
-    if (head_dim == 128)
-        tiles == 1 ? cached_attention_kernel<128, 1><<<blocks, threads, 0, stream>>>(a) : cached_attention_kernel<128, 2><<<blocks, threads, 0, stream>>>(a);
-    else
-        tiles == 1 ? cached_attention_kernel<64, 1><<<blocks, threads, 0, stream>>>(a) : cached_attention_kernel<64, 2><<<blocks, threads, 0, stream>>>(a);
+    const auto kernel = head_dim == 128 ? tiles == 1 ? cached_attention_kernel<128, 1> : cached_attention_kernel<128, 2>
+                                        : tiles == 1 ? cached_attention_kernel<64, 1> : cached_attention_kernel<64, 2>;
+    kernel<<<blocks, threads, 0, stream>>>(s.lengths, s.table, s.cu, q.p, q.token, q.head, kv_heads, group, a);
     if (cut) {
         const int most = units < PARTS ? (int)units : PARTS, used = s.cu || group > rows ? rows : group;
         const int waves_a_row = (int64_t)most * used <= 4096 ? JOIN_WAVES : 1;

@@ -88,11 +88,13 @@ struct Item {
 struct Items {
     static constexpr int SORTED = 32;
     const PromptArgs &a;
-    int blocks, before;                        // of the lane's sequence, and those that come before them
-    __device__ explicit Items(const PromptArgs &args) : a(args), blocks(0), before(0)
+    Span own;                                  // the lane's sequence, its blocks and the blocks that come before them
+    int blocks, before;
+    __device__ explicit Items(const PromptArgs &args) : a(args), own{0, 0}, before(0)
     {
         const int lane = lane_id();
-        if (lane < a.seq.count) blocks = (new_tokens(a.seq, lane).n + QT - 1) / QT;
+        if (lane < a.seq.count) own = new_tokens(a.seq, lane);
+        blocks = (own.n + QT - 1) / QT;
         const int order = blocks * 64 + 63 - lane;       // of two with as many blocks the first one comes first; 2^17 blocks at most
         if (a.seq.count <= SORTED)
             for (int j0 = 0; j0 < a.seq.count; j0 += 8)  // eight at a time: one by one each waits for the one before, 180 cycles
@@ -107,18 +109,20 @@ struct Items {
         const int block = index / a.heads, slot = index % a.heads;
         Item i = {0, 0, 0, slot};
         if (a.heads % 8 == 0) i.head = slot % 8 * (a.heads / 8) + slot / 8;      // an XCD, every eighth workgroup, gets heads that share keys and values
-        Found f;                                       // the place is from the sequence's last block on
+        int place;                                     // from the sequence's last block on
         if (a.seq.count <= SORTED) {
             const uint64_t hit = __ballot(block >= before && block < before + blocks);
             if (!hit) return i;
-            f.sequence = __builtin_ctzll(hit), f.place = block - __builtin_amdgcn_readlane(before, f.sequence);
+            const int b = __builtin_ctzll(hit);
+            place = block - __builtin_amdgcn_readlane(before, b);
+            i.begin = __builtin_amdgcn_readlane(own.begin, b), i.n = __builtin_amdgcn_readlane(own.n, b);
         } else {
-            f = find_sequence(a.seq.count, block, [&](int b) { return (new_tokens(a.seq, b).n + QT - 1) / QT; });
+            const Found f = find_sequence(a.seq.count, block, [&](int b) { return (new_tokens(a.seq, b).n + QT - 1) / QT; });
             if (f.sequence < 0) return i;
+            const Span span = new_tokens(a.seq, uniform(f.sequence));
+            place = uniform(f.place), i.begin = uniform(span.begin), i.n = uniform(span.n);
         }
-        const Span span = new_tokens(a.seq, uniform(f.sequence));
-        i.begin = uniform(span.begin), i.n = uniform(span.n);
-        i.row0 = ((i.n + QT - 1) / QT - 1 - uniform(f.place)) * QT;
+        i.row0 = ((i.n + QT - 1) / QT - 1 - place) * QT;
         return i;
     }
 };
@@ -129,8 +133,11 @@ struct Halves {
 };
 
 template <int D>
-__global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const PromptArgs a)
+__global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const int32_t *cu, int32_t count, int32_t tokens, int32_t heads, int32_t group, const PromptArgs rest)
 {
+    // what a workgroup needs first comes with the dispatch
+    PromptArgs a = rest;
+    a.seq.cu = cu, a.seq.count = count, a.seq.tokens = tokens, a.heads = heads, a.group = group;
     constexpr int KS = D / 16, DB = D / 32, ROW = D * 2, TILE = KTILE * ROW, GRANULES = D / 8;
     constexpr int COPIES = TILE / 1024 / 4, ROWS_PER_COPY = 1024 / ROW;        // a copy: 1 KB, 16 bytes a lane
     __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][TILE];         // [stage][keys, values]
@@ -381,8 +388,8 @@ hipError_t launch_prompt_attention(Heads q, Heads k, Heads v, const Sequences &s
     if (blocks > s.tokens) blocks = s.tokens;
     if (blocks * heads > 1 << 23) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)(blocks * heads));
-    if (head_dim == 128) prompt_attention_kernel<128><<<grid, dim3(256), 0, stream>>>(a);
-    else prompt_attention_kernel<64><<<grid, dim3(256), 0, stream>>>(a);
+    if (head_dim == 128) prompt_attention_kernel<128><<<grid, dim3(256), 0, stream>>>(s.cu, s.count, s.tokens, heads, a.group, a);
+    else prompt_attention_kernel<64><<<grid, dim3(256), 0, stream>>>(s.cu, s.count, s.tokens, heads, a.group, a);
     return hipGetLastError();
 }
 
