@@ -64,7 +64,7 @@ struct Shares {
     __device__ explicit Shares(const DecodeArgs &args) : a(args), first{0, 0}, most(1 << 29)
     {
         if (!a.parts && !a.seq.cu) {           // as many units of every sequence, which it takes no lengths to know
-            items = a.most_items;
+            items = a.seq.count * ((a.group + ROWS - 1) / ROWS) * a.kv_heads;
             return;
         }
         first = shape_of<ROWS>(a, lane_id());
@@ -89,7 +89,7 @@ struct Shares {
 };
 
 struct Unit {
-    int sequence, head, tile, part, parts, slot;      // slot: where the part's results go
+    int sequence, head, tile, part, parts, slot;      // sequence -1: there is none; slot: where the part's results go
 };
 // Item `item` of the list: first the parts of units that are cut, then whole units
 template <int ROWS>
@@ -111,7 +111,8 @@ __device__ inline Unit find_unit(const DecodeArgs &a, const Shares<ROWS> &shares
             const Shape s = shares.shape(b);
             return shares.cuts(s) > 1 ? 0 : s.tiles * a.kv_heads;
         });
-    const int b = uniform(max(f.sequence, 0)), place = uniform(f.place);
+    if (f.sequence < 0) return {-1, 0, 0, 0, 1, item};
+    const int b = uniform(f.sequence), place = uniform(f.place);
     const int parts = uniform(shares.cuts(shares.at(b))), unit = place / parts;
     return {b, unit % a.kv_heads, unit / a.kv_heads, place % parts, parts, item};
 }
@@ -177,6 +178,7 @@ __global__ __launch_bounds__(64 * waves_of(RT), 2) void cached_attention_kernel(
     const Shares<ROWS> shares(a);
     for (int item = blockIdx.x; item < shares.items; item += gridDim.x) {
     const Unit u = find_unit<ROWS>(a, shares, item);
+    if (u.sequence < 0) return;
     if (item != (int)blockIdx.x) __syncthreads();             // LDS is free again
     int thread = threadIdx.x;
     asm volatile("" : "+v"(thread));             // what follows from it is not kept from part to part: there are no registers for that

@@ -110,6 +110,20 @@ def test_a_wide_table_of_short_sequences(H, J, D, tokens):
     check(out, *expected(q, new, lengths, table, codes, scales, D ** -0.5), D)
 
 
+@pytest.mark.parametrize("H,J,D,B", [(8, 1, 64, 5), (12, 4, 128, 33), (9, 3, 64, 70), (20, 1, 128, 3), (40, 40, 64, 2)])
+@pytest.mark.parametrize("tokens", [1, 3])
+def test_no_row_behind_the_tokens_is_written(H, J, D, B, tokens):
+    """The host's bound of row tiles is higher than their number where a tile is not full: there is no sequence, and no output, behind the last."""
+    lengths, new = [7 + 13 * b % 90 for b in range(B)], [tokens] * B
+    g = torch.Generator(device="cuda").manual_seed(B)
+    q, _, _ = projection(g, sum(new), H, J, D)
+    table, codes, scales = filled(lengths, J, D, B)
+    out = torch.full((4 * B * tokens + 64, H, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    fptq.fptq_cached_attention(q, cache_of(codes, scales), device(table), device(lengths), device(starts(new)) if tokens > 1 else None, out=out)
+    check(out[:sum(new)], *expected(q, new, lengths, table, codes, scales, D ** -0.5), D)
+    assert (out[sum(new):] == 7).all()
+
+
 def test_tokens_before_the_first_key_get_zeros():
     g = torch.Generator(device="cuda").manual_seed(4)
     q, _, _ = projection(g, 9, 4, 2, 64)
