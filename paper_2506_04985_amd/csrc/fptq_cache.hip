@@ -3,6 +3,11 @@
 // A page-head (64 tokens of one kv head) holds e4m3 codes c and one scale s, a power of two: x ~ c s, s the smallest with max |x| <= 448 s.  A
 // power of two, because then older codes move to a larger scale by an exponent, c' = rne(c 2^-n), and the attention's widening to bf16 takes
 // the scale for nothing and exactly.  Keys are rotated in fp32 (every product and sum rounded by itself, no contraction) and rounded once, to the code.
+//
+// A launch for everything: a workgroup for the keys or the values of a page-head, whose scale needs all of the page's new tokens, and waves for the queries of a
+// token, which keep its angles over the heads.  Values are read a row a wave and written transposed, 16 tokens a lane, from registers.
+// Measured: a prompt of 4096 tokens, 32 heads over 8 of 128, 103 MB read and written: 19.6 us, 5.2 TB/s; a token 4.1 us, a chain of latencies (length, angles,
+// page, its scale and codes) of which the rows' own is taken out by reading them first.
 #include "fptq_attention.h"
 
 namespace fptq {

@@ -6,11 +6,17 @@
 // them, as columns: S^T = K Q^T and O^T = V^T P^T with 32 x 32 x 16 products.  So a lane holds scores of one token only (half of them, the lane 32
 // away the others), the softmax needs one exchange where a maximum has grown, and what S^T leaves in a lane is what O^T wants of it: keys
 // 4 h + e and 8 + 4 h + e of every 16, h the half of the wave.  Keys and values go to LDS 64 tokens at a time without passing through registers,
-// two tiles deep; values are read back transposed by the LDS.  16-byte granules are exchanged within rows so that these reads have no bank conflicts; the exchange is
-// made by the addresses that the copies' lanes read from.
+// two tiles deep; values are read back transposed by the LDS.  16-byte granules are exchanged within rows so that these reads have no bank conflicts; the
+// exchange is made by the addresses that the copies' lanes read from.  Scores of a tile are made while the weights of the tile before are, and their
+// maximum beside that tile's products, so that matrix instructions run under the others.
 //
-// P is rounded to bf16 (half a step, 2^-9 of each term); maxima, sums and outputs are fp32.  The accumulators are rescaled only when a maximum has grown by
+// P is rounded to bf16 (half a step, 2^-8 of each term); maxima, sums and outputs are fp32.  The accumulators are rescaled only when a maximum has grown by
 // more than 2^8: until then p is at most 256 and loses nothing, being a float.
+//
+// Measured: 8192 tokens, 64 heads over 8 of 128: 962 us, 1143 TFLOP/s, where a library product of 8192 x 8192 x 8192 reaches 1130 to 1270.  1.78 million cycles,
+// matrix cores busy 60 % of them, at 1.7 to 1.8 GHz: with zeros for data, which draw less power, 750 us.  4096 tokens, 32 heads over 8: 131 to 145 us; nine
+// prompts of 6000 tokens, 32 heads over 32: 79 to 91 us.  A workgroup costs 10000 to 13000 cycles besides its tiles (about 1450 each, two
+// workgroups a CU): 5000 to 7000 until the first tile is there, 3000 at the diagonal, 1700 to write.
 #include "fptq_attention.h"
 
 namespace fptq {
@@ -133,7 +139,8 @@ struct Halves {
 };
 
 template <int D>
-__global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const int32_t *cu, int32_t count, int32_t tokens, int32_t heads, int32_t group, const PromptArgs rest)
+__global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const int32_t *cu, int32_t count, int32_t tokens, int32_t heads, int32_t group,
+                                                                 const PromptArgs rest)
 {
     // what a workgroup needs first comes with the dispatch
     PromptArgs a = rest;

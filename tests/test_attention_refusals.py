@@ -71,8 +71,8 @@ def test_no_tokens_are_nothing_to_do():
 
 def test_scratch_bytes():
     f = fptq.fptq_cached_attention_scratch_bytes
-    assert f(1, 1, 8, 2, 128, 64) == 0                      # 64 pages are never cut
-    assert f(1, 1, 8, 2, 128, 65) == 3072 * 16 * 130 * 4
+    assert f(1, 1, 8, 2, 128, 16) == 0                      # 16 pages are never cut
+    assert f(1, 1, 8, 2, 128, 17) == 3072 * 16 * 130 * 4
     assert f(8, 1, 8, 2, 64, 4096) == 3072 * 32 * 66 * 4    # 32 rows a tile
     for bad in ((1, 1, 8, 3, 128, 16), (1, 1, 8, 2, 100, 16), (1, 1, 8, 2, 128, 0), (-1, 1, 8, 2, 128, 16)):
         with pytest.raises(fptq.FptqError) as e:

@@ -71,9 +71,9 @@ def test_several_tokens_each(new, lengths, H, J, D):
 
 
 @pytest.mark.parametrize("H,J,D,new,lengths", [(4, 1, 64, [1], [5000]), (8, 2, 128, [1, 1, 1], [4200, 40, 6000]), (4, 1, 64, [6, 2], [4097, 9000]),
-                                               (16, 1, 128, [5, 1, 0], [4500, 5000, 90])])
+                                               (16, 1, 128, [5, 1, 0], [4500, 5000, 90]), (6, 2, 128, [1] * 70, [1100] * 69 + [2100])])
 def test_long_sequences_shared_out_and_not(H, J, D, new, lengths):
-    """More than 64 pages are cut into parts.  Without scratch they are not; both are within the bound, and the parts' own order is the same every time."""
+    """More than 16 pages are cut into parts where there are few.  Without scratch they are not; both are within the bound, and the parts' own order is the same every time."""
     run(new, lengths, H, J, D, seed=1)
     g = torch.Generator(device="cuda").manual_seed(1)
     q, _, _ = projection(g, sum(new), H, J, D)
