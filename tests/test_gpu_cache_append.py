@@ -112,6 +112,13 @@ def test_wide_heads(rope_dims):
     run([70, 3, 140], [10, 0, 60], 6, 2, 128, rope_dims, True, seed=3)
 
 
+def test_many_sequences():
+    """More than a wave's 64, with none, one and several new tokens."""
+    rng = np.random.default_rng(11)
+    run([int(n) for n in rng.integers(0, 4, 150)], [int(n) for n in rng.integers(0, 130, 150)], 2, 1, 64, 64, False, seed=11)
+    run([1] * 150, [int(n) for n in rng.integers(0, 130, 150)], 2, 1, 64, 32, True, seed=12, with_cu=False)
+
+
 @pytest.mark.parametrize("spread", [0.0, 1e-4, 300.0])
 def test_scales(spread):
     """Zeros (the smallest scale in a new page, the older one in another), values far below the older ones and far above them."""

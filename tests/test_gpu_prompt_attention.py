@@ -26,6 +26,17 @@ def test_packed_prompts(new, H, J, D):
     check(out, *expected(q, k, v, new, D ** -0.5), D)
 
 
+@pytest.mark.parametrize("B", [8, 9, 32, 33, 64, 65, 130])
+def test_many_prompts(B):
+    """Up to 32 sequences are sorted by length, more are taken in their order, 64 at a time."""
+    new = [int(n) for n in np.random.default_rng(B).integers(0, 150, B)]
+    new[B // 2] = 300
+    g = torch.Generator(device="cuda").manual_seed(B)
+    q, k, v = projection(g, sum(new), 3, 1, 64)
+    out = fptq.fptq_prompt_attention(q, k, v, device(starts(new)))
+    check(out, *expected(q, k, v, new, 0.125), 64)
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_a_long_prompt_with_large_scores(D):
     """Scores far apart, so that the running maximum grows often and by much."""
