@@ -34,7 +34,7 @@ struct PromptArgs {
 };
 
 constexpr float NONE = -__builtin_inff();
-constexpr int QK_AHEAD = 4, PV_AHEAD = 4;
+constexpr int AHEAD = 4;                       // products whose operands are read from LDS before the first one (2, 3 and 6: the same within 1 %)
 constexpr int QT = 128, KTILE = 64;            // tokens of a workgroup, keys of a tile
 
 __device__ inline float other_half_max(float v)
@@ -283,23 +283,25 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const int32_t 
         v8bf p[4];
         scores(stage ^ 1, next);
         weights(ALL, now, p);
-        __builtin_amdgcn_sched_group_barrier(0x100, QK_AHEAD, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
 #pragma unroll
         for (int i = 0; i < 2 * KS; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x002, 112 / (2 * KS), 0);
         }
+        asm volatile("" : "+v"(l));                           // here and not after the barrier, where nothing runs under it
         __builtin_amdgcn_sched_barrier(0);
         products(ALL, stage, p);
         top = largest(ALL, next);
-        __builtin_amdgcn_sched_group_barrier(0x100, 2 * PV_AHEAD, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * AHEAD, 0);
 #pragma unroll
         for (int i = 0; i < 4 * DB; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
             __builtin_amdgcn_sched_group_barrier(0x002, 32 / (4 * DB), 0);
         }
+        asm volatile("" : "+v"(top));
         __builtin_amdgcn_sched_barrier(0);
     };
     int tile = 0;

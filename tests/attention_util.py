@@ -2,8 +2,6 @@
 import numpy as np
 import torch
 
-from paper_2506_04985_amd import binding as fptq
-
 PAGE = 64
 
 
@@ -57,6 +55,3 @@ def check(got, out, mass, terms, D):
     far = np.abs(got - out)[finite] / tolerance(out, mass, terms, D)[finite]
     assert far.size == 0 or far.max() <= 1.0, f"{far.max()} of the bound"
 
-
-def reference_cache(pages, J, D):
-    return fptq.Cache.empty(pages, J, D)
