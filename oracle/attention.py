@@ -75,7 +75,7 @@ def from_values_page(flat, D):
 
 def attention(q, k, v, scale, keys=None):
     """q [n, H, D], k and v [m, J, D]: the last query is at the last key, or token i sees the first keys[i]; a query that sees nothing gets zeros.
-    `seen` [m], optional within keys, is not part of this: unseen tokens are left out by the caller.  Returns (out, the mean of |v| under the softmax, the
+    Returns (out, the mean of |v| under the softmax, the
     largest sum |q k| scale of a row): what error bounds are made of."""
     n, H, D = q.shape
     m, J = k.shape[0], k.shape[1]
