@@ -258,11 +258,12 @@ __global__ __launch_bounds__(64 * waves_of(RT), 2) void cached_attention_kernel(
         int id = look_up(0);
         for (int i0 = 0; i0 < mine; i0 += 64) {
             if (i0) id = look_up(i0);
-            // A number outside the pool is no page: its tokens are not seen.
+            // A number outside the pool is no page: its tokens are not seen.  Page 0's codes are loaded in its place and become NONE and zeros; their scale is 1
+            // and not page 0's, which may never have been written: zero widened by a scale of NaN is NaN.
             if (i0 + lane >= mine || id < 0 || id >= a.cache.pages) id = -1;
             float ks = 1.0f, vs = 1.0f;
-            if (i0 + lane < mine) {
-                const int64_t at = (int64_t)max(id, 0) * a.kv_heads + u.head;
+            if (id >= 0) {
+                const int64_t at = (int64_t)id * a.kv_heads + u.head;
                 ks = a.cache.ks[at], vs = a.cache.vs[at];
             }
             const int count = min(mine - i0, 64);

@@ -163,6 +163,28 @@ def test_page_numbers_outside_the_pool_are_not_seen():
         check(out[b:b + 1], *oracle.attention(host(q[b:b + 1]), k[seen], v[seen], 0.125), 64)
 
 
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), 0.0])
+@pytest.mark.parametrize("H,J,D,tokens,more", [(4, 2, 64, 1, 0), (16, 1, 128, 1, 0), (8, 1, 64, 4, 0), (40, 2, 128, 1, 0), (4, 1, 64, 1, 40)])
+def test_page_numbers_outside_the_pool_whatever_the_first_page_holds(scale, H, J, D, tokens, more):
+    """Page 0 belongs to nobody, and neither its codes nor its scales were ever written: pages that are not there take nothing of it."""
+    g = torch.Generator(device="cuda").manual_seed(12)
+    q, _, _ = projection(g, 2 * tokens, H, J, D)
+    lengths = [300 + more * PAGE, 130]
+    table, codes, scales = filled(lengths, J, D, 12)
+    codes = np.concatenate([np.full_like(codes[:, :1], 127), codes], 1)
+    scales = np.concatenate([np.full_like(scales[:, :1], scale), scales], 1)
+    table += 1
+    pool = codes.shape[1]
+    bad = table.copy()
+    bad[0, 1], bad[0, 3], bad[1, 0] = -1, pool, 0x7FFFFFFF
+    out = fptq.fptq_cached_attention(q, cache_of(codes, scales), device(bad), device(lengths), device([0, tokens, 2 * tokens]) if tokens > 1 else None)
+    for b, gone in ((0, [1, 3]), (1, [0])):
+        k, v = tokens_of(table[b], codes, scales, lengths[b])
+        seen = ~np.isin(np.arange(lengths[b]) // PAGE, gone)
+        rows = slice(b * tokens, (b + 1) * tokens)
+        check(out[rows], *oracle.attention(host(q[rows]), k[seen], v[seen], D ** -0.5), D)
+
+
 def test_a_length_beyond_the_table():
     g = torch.Generator(device="cuda").manual_seed(7)
     q, _, _ = projection(g, 1, 2, 2, 64)
