@@ -238,8 +238,8 @@ int fptq_w4a4_linear_ref(const void *xq_packed, const void *w_packed, int64_t M,
  * What a decoder layer does between its QKV and its O projection: rotate queries and keys by position, keep keys and values in a paged
  * 8-bit cache, and attend, over whole prompts or over the cache.  The calls work on `tokens` new tokens of `sequences` sequences, packed
  * one sequence after the other.
- *   tokens                      up to 2^24; 0: nothing is done
- *   heads, kv_heads, head_dim   query heads, a multiple of kv_heads; head h reads key and value head h / (heads / kv_heads); head_dim 64 or 128
+ *   tokens                      up to 2^24, as sequences are; 0: nothing is done
+ *   heads, kv_heads, head_dim   query heads, up to 4096 and a multiple of kv_heads; head h reads key and value head h / (heads / kv_heads); head_dim 64 or 128
  *   fptq_heads                  bf16 rows: value d of head h of token t is data[t * token_stride + h * head_stride + d].  Strides are in
  *                               values, multiples of 8 from 0 to 2^24 - 8; data is 16-byte aligned.  So parts of the QKV projection's rows serve as they are.
  *   cu                          device, int32 [sequences + 1]: sequence b's tokens are cu[b] .. cu[b + 1] - 1 (none is allowed); NULL: one token
@@ -248,6 +248,13 @@ int fptq_w4a4_linear_ref(const void *xq_packed, const void *w_packed, int64_t M,
  *   table, table_width          device, int32 [sequences x table_width]: pages of a sequence in order, 64 tokens each
  * Array contents that cannot be checked before the launch are checked on the device: a page number outside the cache, or a position that
  * the table does not reach, is no page (nothing is written there and nothing there is seen); a position outside the rotation's table makes NaN.
+ *
+ * Together the sizes are limited by what one launch may hold.  A call beyond it is refused (FPTQ_ERR_SHAPE) and is to be made in parts, of whole
+ * sequences.  What is served:
+ *   fptq_cache_append      2 * kv_heads * min(tokens, tokens / 64 + 2 * sequences) + tokens / 4 up to 2^24 - 2048
+ *   fptq_cached_attention  kv_heads * min(rows, rows / R + sequences) up to 2^23, with scratch 2^23 - 3072; rows is tokens * heads / kv_heads,
+ *                          R 32 where rows are more than 16 * sequences and 16 where they are not
+ *   fptq_prompt_attention  heads * min(tokens, tokens / 128 + sequences) up to 2^23 (2^24 tokens of up to 63 heads, in one prompt)
  */
 typedef struct {
     const void *data;
@@ -286,7 +293,8 @@ int fptq_cache_append(const fptq_heads *q, const fptq_heads *k, const fptq_heads
  * out = softmax(scale * q k^T) v over the cache, bf16 [tokens x heads x head_dim] contiguous.  A token sees its sequence up to itself; one at a
  * negative position sees nothing and gets zeros.
  *   scratch    device, 256-byte aligned, at least fptq_cached_attention_scratch_bytes(...) bytes (which may be 0), or NULL.  With it, long sequences are
- *              shared out to many compute units.  Its contents need no initialisation and mean nothing afterwards.  Calls that share it must not overlap in time.
+ *              shared out to many compute units.  Too small: as NULL.  Its contents need no initialisation and mean nothing afterwards.  Calls that share
+ *              it must not overlap in time.
  */
 int64_t fptq_cached_attention_scratch_bytes(int64_t tokens, int64_t sequences, int heads, int kv_heads, int head_dim, int64_t table_width);
 int fptq_cached_attention(const fptq_heads *q, int64_t tokens, int64_t sequences, int heads, int kv_heads, int head_dim, float scale,

@@ -377,16 +377,16 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs a)
 hipError_t launch_cache_append(Heads q, Heads k, Heads v, const Sequences &s, int heads, int kv_heads, int head_dim, const float *rope, int64_t positions,
                                int rope_dims, bool interleaved, const Cache &cache, uint16_t *q_out, uint16_t *k_out, hipStream_t stream)
 {
-    const DeviceInfo *info;
-    hipError_t e = device_info(&info);
-    if (e != hipSuccess) return e;
     AppendArgs a = {q, k, v, s, cache, rope, positions, q_out, k_out, heads, kv_heads, rope_dims, 0, 0};
     // a sequence of n new tokens touches at most n / 64 + 2 pages, and no more than n
     a.page_slots = s.cu ? (int)(s.tokens < s.tokens / PAGE + 2 * (int64_t)s.count ? s.tokens : s.tokens / PAGE + 2 * (int64_t)s.count) : s.count;
     const int groups = (heads * (head_dim / 16) + 63) / 64;
     a.query_parts = (int64_t)s.tokens * groups <= 4096 ? groups : 1;
     const int64_t blocks = (int64_t)a.page_slots * kv_heads * 2 + ((int64_t)s.tokens * a.query_parts + 3) / 4;
-    if (blocks * 256 >= (int64_t)1 << 32) return hipErrorInvalidConfiguration;
+    if (blocks * 256 >= (int64_t)1 << 32) return hipErrorInvalidConfiguration;      // before the device is asked for anything
+    const DeviceInfo *info;
+    hipError_t e = device_info(&info);
+    if (e != hipSuccess) return e;
     const auto kernel = head_dim == 128 ? interleaved ? cache_append_kernel<128, true> : cache_append_kernel<128, false>
                                         : interleaved ? cache_append_kernel<64, true> : cache_append_kernel<64, false>;
     kernel<<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a);

@@ -539,16 +539,16 @@ int64_t cached_attention_scratch_bytes(int64_t tokens, int64_t sequences, int he
 hipError_t launch_cached_attention(Heads q, const Sequences &s, int heads, int kv_heads, int head_dim, float scale, const Cache &cache, uint16_t *out,
                                    uint8_t *scratch, int64_t scratch_bytes, hipStream_t stream)
 {
-    const DeviceInfo *info;
-    hipError_t e = device_info(&info);
-    if (e != hipSuccess) return e;
     const int group = heads / kv_heads, tiles = row_tiles(s.tokens, s.count, group), rows = 16 * tiles;
     const int64_t units = most_units(s.tokens, s.count, group, kv_heads, rows);
     const int64_t need = cached_attention_scratch_bytes(s.tokens, s.count, heads, kv_heads, head_dim, s.table_width);
     const bool cut = need > 0 && scratch && scratch_bytes >= need;
     DecodeArgs a = {q, s, cache, out, cut ? (float *)scratch : nullptr, heads, kv_heads, group, scale * 1.44269504088896341f, 0, least_share(units)};
     const int64_t items = units + (cut ? most_cut(units, s.table_width) : 0), grid = items < MAX_GRID || (head_dim == 128 && tiles == 2) ? items : MAX_GRID;
-    if (items > 1 << 23) return hipErrorInvalidConfiguration;
+    if (items > 1 << 23) return hipErrorInvalidConfiguration;      // before the device is asked for anything; n * group fits in 32 bits then
+    const DeviceInfo *info;
+    hipError_t e = device_info(&info);
+    if (e != hipSuccess) return e;
     a.most_items = (int)items;
     const dim3 threads(64 * waves_of(tiles)), blocks((unsigned)grid);
     const auto kernel = head_dim == 128 ? tiles == 1 ? cached_attention_kernel<128, 1> : cached_attention_kernel<128, 2>

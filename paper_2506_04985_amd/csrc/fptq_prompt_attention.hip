@@ -389,13 +389,13 @@ __global__ __launch_bounds__(256, 2) void prompt_attention_kernel(const int32_t 
 hipError_t launch_prompt_attention(Heads q, Heads k, Heads v, const Sequences &s, int heads, int kv_heads, int head_dim, float scale, uint16_t *out,
                                    hipStream_t stream)
 {
-    const DeviceInfo *info;
-    hipError_t e = device_info(&info);
-    if (e != hipSuccess) return e;
     const PromptArgs a = {q, k, v, s, out, heads, heads / kv_heads, scale * 1.44269504088896341f};
     int64_t blocks = s.tokens / QT + (int64_t)s.count;               // of n tokens: n / QT + 1 at most
     if (blocks > s.tokens) blocks = s.tokens;
-    if (blocks * heads > 1 << 23) return hipErrorInvalidConfiguration;
+    if (blocks * heads > 1 << 23) return hipErrorInvalidConfiguration;      // before the device is asked for anything
+    const DeviceInfo *info;
+    hipError_t e = device_info(&info);
+    if (e != hipSuccess) return e;
     const dim3 grid((unsigned)(blocks * heads));
     if (head_dim == 128) prompt_attention_kernel<128><<<grid, dim3(256), 0, stream>>>(s.cu, s.count, s.tokens, heads, a.group, a);
     else prompt_attention_kernel<64><<<grid, dim3(256), 0, stream>>>(s.cu, s.count, s.tokens, heads, a.group, a);

@@ -65,6 +65,39 @@ def test_prompt_attention(change, code):
     assert b"fptq_prompt_attention" in fptq.lib().fptq_last_error()
 
 
+# Sizes that are within their own limits each and together ask for more workgroups than a launch may have (include/fptq.h states how many), refused
+# before the device is asked for anything.  No call here is just within them: its pointers are made up, and it would be launched where there is a GPU.
+BIG = 1 << 24
+
+
+@pytest.mark.parametrize("change", [{"tokens": 1 << 20, "sequences": 1 << 20, "heads": 8, "kv_heads": 8}, {"tokens": BIG, "sequences": BIG},
+                                    {"tokens": BIG, "sequences": 1, "heads": 32, "kv_heads": 32, "cu": P}, {"tokens": 4096, "sequences": 4096, "heads": 4096, "kv_heads": 4096}])
+def test_cache_append_of_too_much(change):
+    assert append(**change) == -2
+    assert b"fptq_cache_append: too many" in fptq.lib().fptq_last_error()
+
+
+@pytest.mark.parametrize("more", [{}, {"scratch": P, "bytes": 1 << 40}])
+@pytest.mark.parametrize("change", [{"tokens": 1 << 21, "sequences": 1 << 21, "heads": 8, "kv_heads": 8, "width": 100}, {"tokens": BIG, "sequences": 1, "heads": 64, "kv_heads": 8, "cu": P},
+                                    {"tokens": BIG, "sequences": 1, "heads": 4096, "kv_heads": 1, "cu": P}])
+def test_cached_attention_of_too_much(change, more):
+    assert cached(**change, **more) == -2
+    assert b"fptq_cached_attention: too many" in fptq.lib().fptq_last_error()
+
+
+def test_the_parts_of_cached_attention_count_too():
+    """Without scratch nothing is cut, and 2^23 rows are served; with it there can be 3072 parts beside them."""
+    assert cached(tokens=1 << 20, sequences=1 << 20, heads=8, kv_heads=8, width=100, scratch=P, bytes=1 << 40) == -2
+    assert b"fptq_cached_attention: too many" in fptq.lib().fptq_last_error()
+
+
+@pytest.mark.parametrize("change", [{"tokens": BIG, "heads": 64}, {"tokens": BIG, "sequences": BIG}, {"tokens": 1 << 20, "sequences": 1 << 20, "heads": 16},
+                                    {"tokens": 4096, "sequences": 4096, "heads": 4096}])
+def test_prompt_attention_of_too_much(change):
+    assert prompt(**change) == -2
+    assert b"fptq_prompt_attention: too many" in fptq.lib().fptq_last_error()
+
+
 def test_no_tokens_are_nothing_to_do():
     assert append(tokens=0, cu=P) == 0 and cached(tokens=0, cu=P) == 0 and prompt(tokens=0) == 0
 
