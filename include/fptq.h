@@ -283,7 +283,8 @@ typedef struct {
  *   k_out      the same of the keys, [tokens x kv_heads x head_dim], or NULL
  * Codes are rounded once, from the fp32 keys.  A page's scale is the smallest power of two s with max |x| <= 448 s over its tokens (2^-100 at least); new
  * tokens that begin in the middle of a page keep the scale it has or raise it, and then its older codes are rounded again.  Values that are not finite
- * do not count for the scale and are stored as NaN.  No page may belong to two sequences that are appended to.
+ * do not count for the scale and are stored as NaN.  Codes of the largest scale, 2^120, end at 240: 256 * 2^120 is infinite in bf16.
+ * No page may belong to two sequences that are appended to.
  */
 int fptq_cache_append(const fptq_heads *q, const fptq_heads *k, const fptq_heads *v, int64_t tokens, int64_t sequences, int heads, int kv_heads,
                       int head_dim, const float *rope, int64_t positions, int rope_dims, int interleaved, const fptq_cache *cache, const int32_t *table,

@@ -19,6 +19,11 @@ __device__ inline uint32_t scale_bits(uint32_t largest) { return (uint32_t)max((
 // bits of 1 / s of a power of two between 2^-126 and 2^126
 __device__ inline float reciprocal_of(uint32_t scale) { return __uint_as_float((254u << 23) - scale); }
 
+// What a value in units of the scale is held to where the scale is the largest there is: from 248 on the nearest code would be 256, which is worth
+// 2^128 and infinite in the bf16 that the attention widens it to.  240 is within half a step's 2^-4 of all that a float can be there; what is not finite stays so.
+constexpr float LARGEST_SCALE = 0x1p120f;
+__device__ inline float below_infinity(float y) { return fabsf(y) < 256.0f ? fminf(fmaxf(y, -240.0f), 240.0f) : y; }
+
 // |x| as it counts for the scale: what is not finite does not, and is stored as NaN
 __device__ inline uint32_t magnitude(float x)
 {
@@ -261,6 +266,9 @@ __device__ inline void append_keys(const AppendArgs &a, const PageRows &r, int j
             float *const y = x[p];
 #pragma unroll
             for (int e = 0; e < 16; ++e) y[e] *= unit;
+            if (scale == LARGEST_SCALE)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) y[e] = below_infinity(y[e]);
             uint2 lo = {codes(y[0], y[1], y[2], y[3]), codes(y[4], y[5], y[6], y[7])};
             uint2 hi = {codes(y[8], y[9], y[10], y[11]), codes(y[12], y[13], y[14], y[15])};
             *(uint2 *)(to + run.lo / 64 * (PAGE * 64) + row * 64 + run.lo % 64) = lo;
@@ -315,12 +323,14 @@ __device__ inline void append_values(const AppendArgs &a, const PageRows &r, int
     if (last <= first && !raised) return;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
+#pragma unroll
+        for (int t = 0; t < 16; ++t) x[e][t] *= unit;
+        if (scale == LARGEST_SCALE)
+#pragma unroll
+            for (int t = 0; t < 16; ++t) x[e][t] = below_infinity(x[e][t]);
         v4u w;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float *const y = x[e] + 4 * i;
-            w[i] = codes(y[0] * unit, y[1] * unit, y[2] * unit, y[3] * unit);
-        }
+        for (int i = 0; i < 4; ++i) w[i] = codes(x[e][4 * i], x[e][4 * i + 1], x[e][4 * i + 2], x[e][4 * i + 3]);
         if (!whole) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {

@@ -142,6 +142,29 @@ def test_values_that_are_not_finite():
     run([6], [70], 2, 2, 64, 0, False, seed=6, change=change)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("top", [1.9375 * 2.0 ** 127, 1.9921875 * 2.0 ** 127, -1.9921875 * 2.0 ** 127])
+def test_the_largest_values_there_are_stay_finite(top, D):
+    """From 1.9375 * 2^127 on the nearest code, 256, would be worth 2^128, which bf16 does not hold: what reads the cache would make an infinity of it, and NaN
+    of that for tokens that do not see it.  The code below it is 240 / 255 of the largest value, within half a step's 2^-4."""
+    g = torch.Generator(device="cuda").manual_seed(13)
+    q, k, v = projection(g, 2, 2, 1, D)
+    v[1, 0, 3], v[1, 0, D - 1], k[1, 0, 5] = top, -top, top
+    cache = fptq.Cache.empty(1, 1, D)
+    table, lengths, cu = device([[0]]), device([2]), device([0, 2])
+    fptq.fptq_cache_append(q, k, v, None, cache, table, lengths, cu)
+    assert cache.value_scales.item() == cache.key_scales.item() == 2.0 ** 120
+    codes = oracle.e4m3_values()[oracle.from_values_page(cache.value_codes.cpu().numpy().reshape(-1), D)[:2]]
+    keys = oracle.e4m3_values()[oracle.from_keys_page(cache.key_codes.cpu().numpy().reshape(-1), D)[:2]]
+    want = host(v)[:, 0] / 2.0 ** 120
+    assert (np.abs(codes - want) <= np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** -10)).all()
+    assert codes[1, 3] == -codes[1, D - 1] == keys[1, 5] == np.copysign(240.0, top)
+    q.zero_()                                                           # scores of zero: equal weights
+    out = host(fptq.fptq_cached_attention(q, cache, table, lengths, cu))
+    assert (out[0] == 0).all()                                          # its own value, which the page's scale makes 0
+    np.testing.assert_allclose(out[1], np.broadcast_to(codes[1] / 2 * 2.0 ** 120, (2, D)), rtol=2.0 ** -8)
+
+
 def test_pages_outside_the_pool_and_positions_outside_the_tables():
     """Nothing is written there; rows outside the rotation's table are NaN, the others as ever."""
     g = torch.Generator(device="cuda").manual_seed(7)
