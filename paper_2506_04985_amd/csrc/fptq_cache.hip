@@ -6,8 +6,8 @@
 //
 // A launch for everything: a workgroup for the keys or the values of a page-head, whose scale needs all of the page's new tokens, and waves for the queries of a
 // token, which keep its angles over the heads.  Values are read a row a wave and written transposed, 16 tokens a lane, from registers.
-// Measured: a prompt of 4096 tokens, 32 heads over 8 of 128, 103 MB read and written: 19.6 us, 5.2 TB/s; a token 4.1 us, a chain of latencies (length, angles,
-// page, its scale and codes) of which the rows' own is taken out by reading them first.
+// Measured (the kernel; a call among others): a prompt of 4096 tokens, 32 heads over 8 of 128, 103 MB read and written: 19.6 us, 5.2 TB/s; 19.5 to 23.  A token 4.1 us;
+// 5.8 to 6.0: a chain of latencies (length, angles, page, its scale and codes) of which the rows' own is taken out by reading them first.
 #include "fptq_attention.h"
 
 namespace fptq {

@@ -5,7 +5,8 @@
 // in one pass over the cache.  What bounds it is the reading of the cache: 2 D bytes a token and kv head, some 2 G operations a byte.
 //
 // A wave takes a page-head (64 tokens of a kv head) at a time.  The query rows that read it (G heads of every new token) are the columns of the matrix
-// instructions, 16 of them or 32, so nothing of the cache is read twice:  S^T = K Q^T and O^T = V^T P^T.  Codes go from memory to registers 16 bytes a
+// instructions, 16 of them or 32:  S^T = K Q^T and O^T = V^T P^T.  Where the rows fit one such tile nothing of the cache is read twice; of more rows (a group of 40,
+// a chunk of a prompt behind what is cached of it) every tile reads and widens it for itself.  Codes go from memory to registers 16 bytes a
 // lane and are widened to bf16 there, scale included (both exact), two values an instruction; the page's layout is such that each lane's 16 bytes are
 // what the instructions want of it: of keys 16 values of one token; of values the 16 tokens whose scores the lane holds, when row
 // 4 g + i of the b-th 16 of S^T is token 16 g + 4 b + i.  So P^T needs no exchange between lanes and nothing goes through LDS in the loop.
@@ -17,7 +18,8 @@
 // results a second kernel joins.  Everything about lengths is read on the device, so a captured launch serves growing sequences.
 //
 // Measured: 64 sequences of up to 32768 tokens (64 heads over 8, 2.72 GB of codes) 476 us, 5.7 TB/s where a kernel that only reads takes 440 to 454; 32 of up to 4096
-// (163 MB) 36.9 us, reading alone 27.5; short calls are a chain of memory latencies (length, page number, codes): a token behind 333 6.7 us.
+// (163 MB) 36.9 to 38.2 us, reading alone 27.5; short calls are a chain of memory latencies (length, page number, codes): a token behind 333 6.6 us, and 9.0 with a table
+// of 4096 pages, for which the join is launched.  256 new tokens, the last of 8192, 32 heads over 8 of 128, 57 us, 1024 of them 148, where the operations take 30 and 114.
 #include "fptq_attention.h"
 
 namespace fptq {
@@ -36,7 +38,7 @@ __host__ __device__ constexpr int waves_of(int row_tiles) { return row_tiles == 
 // sequences of up to 64 pages, 8 kv heads: 36.9 us uncut, 45.9 with those of more than 48 cut).
 constexpr int LEAST_SHARE = 8, FULL_SHARE = 32;
 static int least_share(int64_t units) { return units >= DEFAULT_CUS ? FULL_SHARE : LEAST_SHARE; }
-constexpr int PARTS = 1536;        // what very many pages are shared out to (64 sequences of up to 32768 tokens 478 us; 1280 483, 1024 507, 2048 490, 1792 499)
+constexpr int PARTS = 1536;        // what very many pages are shared out to (64 sequences of up to 32768 tokens, the only shape timed, 478 us; 1280 483, 1024 507, 2048 490, 1792 499)
 constexpr int MAX_GRID = 1024;     // workgroups; they go on from part to part, so that room in the table for many more parts costs little
 constexpr int JOIN_WAVES = 8;      // of a workgroup of the join
 constexpr int JOINED = 512;        // units that the join's grid is for; if more are cut, its workgroups take several
@@ -234,7 +236,8 @@ __global__ __launch_bounds__(64 * waves_of(RT), 2) void cached_attention_kernel(
             __syncthreads();
         }
         const int first_token = row0 / a.group, last_token = (min(row0 + ROWS, rows) - 1) / a.group;
-        const int all_see = row0 + ROWS <= rows ? max(length - n + 1 + first_token, 0) : 0;      // keys below it need no mask
+        // keys below it need no mask (of a tile that is not full none do: rows that are not there see nothing, so its pages all take the masked way)
+        const int all_see = row0 + ROWS <= rows ? max(length - n + 1 + first_token, 0) : 0;
         const int some_see = max(length - n + 1 + last_token, 0);                                // keys from it on nobody sees
 
         // this part's pages that anybody sees, this wave's among them

@@ -13,10 +13,12 @@
 // P is rounded to bf16 (half a step, 2^-8 of each term); maxima, sums and outputs are fp32.  The accumulators are rescaled only when a maximum has grown by
 // more than 2^8: until then p is at most 256 and loses nothing, being a float.
 //
-// Measured: 8192 tokens, 64 heads over 8 of 128: 962 us, 1143 TFLOP/s, where a library product of 8192 x 8192 x 8192 reaches 1130 to 1270.  1.78 million cycles,
-// matrix cores busy 60 % of them, at 1.7 to 1.8 GHz: with zeros for data, which draw less power, 750 us.  4096 tokens, 32 heads over 8: 131 to 145 us; nine
-// prompts of 6000 tokens, 32 heads over 32: 79 to 91 us.  A workgroup costs 10000 to 13000 cycles besides its tiles (about 1450 each, two
-// workgroups a CU): 5000 to 7000 until the first tile is there, 3000 at the diagonal, 1700 to write.
+// Measured (a call among others, on several boxes; the kernel under the profiler's trace, two batches in turn): 8192 tokens, 64 heads over 8 of 128: 960 to 1005 us; 997
+// to 1022, 1080 to 1145 TFLOP/s, where a library product of 8192 x 8192 x 8192 reaches 1130 to 1270.  1.69 million cycles, matrix cores busy 63 % of them, at
+// 1.7 GHz: with zeros for data, which draw less power, 750 us.  4096 tokens, 32 heads over 8: 131 to 145 us; 142 to 150.  Nine prompts of 6000 tokens together, 32
+// heads over 32: 78 to 91 us; 72 to 77.  With 64 values a head, 32 heads over 8, 4096 and 8192 tokens: 82 and 293 us, where the operations take 61 and 244.
+// A workgroup costs 10000 to 13000 cycles besides its tiles (about 1450 each, two workgroups a CU): 5000 to 7000 until the first tile is there, 3000 at the
+// diagonal, 1700 to write.  So a prompt that leaves CUs idle is as long as its last block's chain: 512, 1024 and 2048 tokens, 32 heads over 8 of 128, 12.4, 21 and 45 us.
 #include "fptq_attention.h"
 
 namespace fptq {
