@@ -15,6 +15,14 @@ pytestmark = pytest.mark.gpu
 POOL = 24
 
 
+@pytest.fixture(autouse=True, scope="module")
+def memory_given_back():
+    """Scratch of 50 MiB here would stay in torch's cache, and a small tensor of a later test in such a segment keeps it: tests/test_gpu_binding.py, which limits
+    the memory, counts on no segment in use having that much left."""
+    yield
+    torch.cuda.empty_cache()
+
+
 def pool_of(J, D, seed):
     rng = np.random.default_rng(seed)
     codes = rng.integers(0, 256, (2, POOL, J, PAGE, D), dtype=np.uint8)
