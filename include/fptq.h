@@ -249,6 +249,9 @@ int fptq_w4a4_linear_ref(const void *xq_packed, const void *w_packed, int64_t M,
  * Array contents that cannot be checked before the launch are checked on the device: a page number outside the cache, or a position that
  * the table does not reach, is no page (nothing is written there and nothing there is seen); a position outside the rotation's table makes NaN.
  *
+ * Scores (scale * q k) are fp32 and may be up to 5 * 10^8 in magnitude.  Beyond it their maximum is rounded by more than an exponential can hold, and rows
+ * become zeros or NaN.
+ *
  * Together the sizes are limited by what one launch may hold.  A call beyond it is refused (FPTQ_ERR_SHAPE) and is to be made in parts, of whole
  * sequences.  What is served:
  *   fptq_cache_append      2 * kv_heads * min(tokens, tokens / 64 + 2 * sequences) + tokens / 4 up to 2^24 - 2048

@@ -13,7 +13,7 @@
 // P is rounded to bf16 (half a step, 2^-8 of each term); maxima, sums and outputs are fp32.  The accumulators are rescaled only when a maximum has grown by
 // more than 2^8: until then p is at most 256 and loses nothing, being a float.
 //
-// Measured (a call among others, on several boxes; the kernel under the profiler's trace, two batches in turn): 8192 tokens, 64 heads over 8 of 128: 960 to 1005 us; 997
+// Measured (a call among others, on several cards; the kernel under the profiler's trace, two batches in turn): 8192 tokens, 64 heads over 8 of 128: 960 to 1005 us; 997
 // to 1022, 1080 to 1145 TFLOP/s, where a library product of 8192 x 8192 x 8192 reaches 1130 to 1270.  1.69 million cycles, matrix cores busy 63 % of them, at
 // 1.7 GHz: with zeros for data, which draw less power, 750 us.  4096 tokens, 32 heads over 8: 131 to 145 us; 142 to 150.  Nine prompts of 6000 tokens together, 32
 // heads over 32: 78 to 91 us; 72 to 77.  With 64 values a head, 32 heads over 8, 4096 and 8192 tokens: 82 and 293 us, where the operations take 61 and 244.

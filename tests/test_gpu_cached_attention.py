@@ -234,3 +234,23 @@ def test_replays_of_a_captured_call_follow_growing_lengths():
         torch.cuda.synchronize()
         assert torch.equal(out, want)
         check(out, *expected(q, [1, 1], [a, b], table, codes, scales, D ** -0.5), D)
+
+
+@pytest.mark.parametrize("H,D,tokens", [(1, 64, 1), (4, 128, 1), (8, 64, 5), (20, 128, 3)])
+@pytest.mark.parametrize("order", ["rising", "falling"])
+def test_the_largest_scores_served(order, H, D, tokens):
+    """Scores of up to 4.9 * 10^8, all of e4m3's positive values apart: all weight is on the largest one seen.  Its weight is rounded to bf16, its sum is not, and
+    the output is rounded."""
+    length = 126
+    table, codes, scales = filled([length], 1, D, 14)
+    flat = np.zeros((2, 1, PAGE, D), np.uint8)
+    flat[0, 0, :, 5], flat[1, 0, :62, 5] = np.arange(1, 65), np.arange(65, 127)
+    if order == "falling":
+        flat[0, 0, :, 5], flat[1, 0, :62, 5] = np.arange(126, 62, -1), np.arange(62, 0, -1)
+    codes[0, table[0, :2]], scales[0] = flat, 1.0
+    q = torch.zeros((tokens, H, D), dtype=torch.bfloat16, device="cuda")
+    q[..., 5] = 2.0 ** 20
+    out = host(fptq.fptq_cached_attention(q, cache_of(codes, scales), device(table), device([length]), device([0, tokens]) if tokens > 1 else None, scale=1.04))
+    _, v = tokens_of(table[0], codes, scales, length)
+    want = v[length - tokens:] if order == "rising" else np.broadcast_to(v[:1], (tokens, 1, D))
+    np.testing.assert_allclose(out, np.broadcast_to(want, (tokens, H, D)), rtol=1.01 * 2 * 2.0 ** -8)

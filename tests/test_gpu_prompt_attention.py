@@ -135,3 +135,18 @@ def test_replays_of_a_captured_call_match_eager_ones():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("order", ["rising", "falling"])
+def test_the_largest_scores_served(order, D):
+    """Scores of up to 4.9 * 10^8, 2^22 apart: all weight is on the largest one seen.  Its weight is rounded to bf16, its sum is not, and the output is rounded."""
+    n = 117
+    g = torch.Generator(device="cuda").manual_seed(14)
+    q, k, v = (torch.zeros((n, 1, D), dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    q[:, 0, 5] = 2048
+    k[:, 0, 5] = (torch.arange(1, n + 1, device="cuda") if order == "rising" else torch.arange(n, 0, -1, device="cuda")) * 2048.0
+    v.copy_(torch.randn(v.shape, device="cuda", generator=g))
+    out = host(fptq.fptq_prompt_attention(q, k, v, device([0, n]), scale=1.0))
+    want = host(v) if order == "rising" else np.broadcast_to(host(v)[:1], (n, 1, D))
+    np.testing.assert_allclose(out, want, rtol=1.01 * 2 * 2.0 ** -8)
