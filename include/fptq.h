@@ -33,6 +33,9 @@
  *   value k in the low nibble when k is even, the high nibble when odd, two's complement.
  *   K is padded to a multiple of 128 with zeros.  fptq_packed_bytes() gives the buffer size.
  *   fptq_unpack() converts back to one int8 per value, so callers never depend on this layout.
+ * Codes of 8 bits lie in the same tiles, 128 bytes a row, of every eight values the even ones first:
+ *   byte(row, k) = ((k / 128) * rows + row) * 128 + (k % 128) / 8 * 8 + (k % 2) * 4 + (k % 8) / 2,
+ *   padded with zeros as well.  fptq_packed8_bytes() gives the size, fptq_unpack8() converts back.
  */
 #ifndef FPTQ_H
 #define FPTQ_H
@@ -47,7 +50,7 @@ extern "C" {
 #define FPTQ_ERR_NULL (-1)  /* a required pointer is NULL                          */
 #define FPTQ_ERR_SHAPE (-2) /* M, N or K is < 1 or too large                       */
 #define FPTQ_ERR_SIZE (-3)  /* a buffer size passed by the caller is too small     */
-#define FPTQ_ERR_MODE (-4)  /* unknown scale mode, or its arguments are missing    */
+#define FPTQ_ERR_MODE (-4)  /* unknown scale mode or type, or its arguments are missing */
 #define FPTQ_ERR_HIP (-5)   /* the HIP runtime refused a launch (see last_error)   */
 #define FPTQ_ERR_VALUE (-6) /* a scalar is not usable (s_a not finite or <= 0)     */
 #define FPTQ_ERR_ALIGN (-7) /* a pointer is misaligned: packed buffers, y_bf16 and
@@ -308,6 +311,55 @@ int fptq_cached_attention(const fptq_heads *q, int64_t tokens, int64_t sequences
 /* out = softmax(scale * q k^T) v of every token over its prompt up to itself, bf16 [tokens x heads x head_dim] contiguous; cu is required. */
 int fptq_prompt_attention(const fptq_heads *q, const fptq_heads *k, const fptq_heads *v, int64_t tokens, int64_t sequences, int heads, int kv_heads,
                           int head_dim, float scale, const int32_t *cu, void *out, void *stream);
+
+/*
+ * Linears whose input four bits cannot carry (a down projection, an output head): activations of 8 bits with a scale for each token, weights of 4
+ * bits with a scale for each group of K values.
+ *
+ * The quantizers: a row u of K values becomes codes in [-127, 127] and one scale, u ~ code * token_scale.  In fp32:
+ *     a = max |u|, at least 2^-100;   code = rne(u * (127 / a));   token_scale = (a * inv) * (1 / 127)
+ * inv is 1 but behind a norm.  A row of zeros has scale 0.  A row with a value that is not finite has codes 0 and scale NaN, so that every output of the token is NaN.
+ *   xq8          device, 16-byte aligned, at least fptq_packed8_bytes(M, K) bytes (xq8_bytes is checked): the codes, in the library's layout
+ *   token_scale  device, fp32 [M]
+ */
+int64_t fptq_packed8_bytes(int64_t rows, int64_t K);
+
+/*
+ * The residual's addition, an RMS norm with its gain, and the quantizer, in one pass: z = x + residual (fp32), u = z * gain, residual_out = bf16(z).
+ *   x_bf16        device, bf16 [M x K]
+ *   residual      device, bf16 [M x K], or NULL: z = x
+ *   gain          device, bf16 [K], or NULL: u = z
+ *   scale_mode    FPTQ_SCALE_RMS: inv = (float)(1 / sqrt(sum z^2 / K + eps)), the sum in fp64; FPTQ_SCALE_NONE: inv = 1
+ *   residual_out  device, bf16 [M x K], or NULL; needs residual, and may be it or x_bf16
+ * The norm's factor is one for a row, so the codes do not depend on it.
+ */
+int fptq_norm_quantize8(const void *x_bf16, const void *residual, const void *gain, int64_t M, int64_t K, int scale_mode, float eps, void *xq8,
+                        int64_t xq8_bytes, float *token_scale, void *residual_out, void *stream);
+
+/*
+ * The gated activation and the quantizer in one pass: u = silu(gate) * up, silu(g) = g / (1 + e^-g) rounded once to fp32 from 64 bits.
+ *   gate, up      device, bf16: value k of token t is gate[t * gate_stride + k].  Strides are in values, at least K (any where M is 1), so the halves of the
+ *                 gate+up projection's rows serve as they are
+ */
+int fptq_gated_quantize8(const void *gate, const void *up, int64_t M, int64_t K, int64_t gate_stride, int64_t up_stride, void *xq8, int64_t xq8_bytes,
+                         float *token_scale, void *stream);
+
+/*
+ * y[t, n] = token_scale[t] * sum_g w_scales[g, n] * (sum over the group's k of code[t, k] * w[n, k]), from one token to long prompts.
+ * The inner sums are exact integers; those of the groups are added in fp32, in an order that the shape alone decides.
+ *   xq8          device, codes from one of the quantizers above
+ *   w_packed     device, packed weights [N x K] from fptq_pack_weights
+ *   group        values of K to a scale: 32, 64 or a multiple of 128 (of K or more: one scale a channel); the last group may be shorter
+ *   w_scales     device, fp32 [ceil(K / group) x N], finite
+ *   y            device, 16-byte aligned, [M x N] row-major of y_type: FPTQ_BF16 or FPTQ_F32
+ */
+#define FPTQ_BF16 0
+#define FPTQ_F32 1
+int fptq_w4a8_linear(const void *xq8, const float *token_scale, const void *w_packed, int64_t M, int64_t N, int64_t K, int64_t group,
+                     const float *w_scales, void *y, int y_type, void *stream);
+
+/* Codes of 8 bits in the library's layout -> int8 [rows x K] row-major (for parity checks and debugging). */
+int fptq_unpack8(const void *packed8, int64_t rows, int64_t K, int8_t *out_int8, void *stream);
 
 /* Library layout -> one int8 per value, [rows x K] row-major (for parity checks and debugging). */
 int fptq_unpack(const void *packed, int64_t rows, int64_t K, int8_t *out_int8, void *stream);

@@ -22,7 +22,8 @@ EXPORTS = ["fptq_version", "fptq_last_error", "fptq_init", "fptq_packed_bytes", 
            "fptq_weight_row_sums", "fptq_w4a4_linear_zp", "fptq_residual_norm_quantize",
            "fptq_w4a4_linear", "fptq_w4a4_linear_ref", "fptq_unpack", "fptq_linear_workspace_bytes", "fptq_w4a4_linear_ws",
            "fptq_w4a4_linear_noalloc", "fptq_linear_scratch_bytes", "fptq_w4a4_linear_scratch",
-           "fptq_cache_append", "fptq_cached_attention_scratch_bytes", "fptq_cached_attention", "fptq_prompt_attention"]
+           "fptq_cache_append", "fptq_cached_attention_scratch_bytes", "fptq_cached_attention", "fptq_prompt_attention",
+           "fptq_packed8_bytes", "fptq_norm_quantize8", "fptq_gated_quantize8", "fptq_w4a8_linear", "fptq_unpack8"]
 TESTING_EXPORTS = ["fptq_set_gemm_tile", "fptq_set_gemm_map", "fptq_set_decode_shape", "fptq_set_linear_prefill",
                    "fptq_linear_launch_plan"]
 
@@ -107,6 +108,16 @@ def lib():
         L.fptq_cached_attention.argtypes = [H, i64, i64, i32, i32, i32, f32, C, p, i64, p, p, p, p, i64, p]
         L.fptq_prompt_attention.restype = i32
         L.fptq_prompt_attention.argtypes = [H, H, H, i64, i64, i32, i32, i32, f32, p, p, p]
+        L.fptq_packed8_bytes.restype = i64
+        L.fptq_packed8_bytes.argtypes = [i64, i64]
+        L.fptq_norm_quantize8.restype = i32
+        L.fptq_norm_quantize8.argtypes = [p, p, p, i64, i64, i32, f32, p, i64, p, p, p]
+        L.fptq_gated_quantize8.restype = i32
+        L.fptq_gated_quantize8.argtypes = [p, p, i64, i64, i64, i64, p, i64, p, p]
+        L.fptq_w4a8_linear.restype = i32
+        L.fptq_w4a8_linear.argtypes = [p, p, p, i64, i64, i64, i64, p, p, i32, p]
+        L.fptq_unpack8.restype = i32
+        L.fptq_unpack8.argtypes = [p, i64, i64, p, p]
         try:
             from . import _native as native      # built next to this file, with the library
         except ImportError as e:                 # only the library was built, or for another torch: the Python path makes the same calls
@@ -522,6 +533,107 @@ def fptq_prompt_attention(q, k, v, cu, scale=None, out=None):
     _dev(cu, torch.int32, "cu")
     out = _rows(out, T, H, D, q, "out")
     _check(lib().fptq_prompt_attention(hq, hk, hv, T, cu.numel() - 1, H, J, D, D ** -0.5 if scale is None else float(scale), _ptr(cu), _ptr(out), _stream()))
+    return out
+
+
+def fptq_packed8_bytes(rows, K):
+    n = lib().fptq_packed8_bytes(rows, K)
+    if n < 0:
+        _check(int(n))
+    return int(n)
+
+
+def _need8(rows, K):
+    return ((K + 127) // 128) * rows * 128
+
+
+def _codes8(M, K, out, token_scale_out, device):
+    """The outputs of a quantizer to 8 bits: the caller's, or new ones."""
+    if out is None:
+        out = torch.empty(_need8(M, K), dtype=torch.int8, device=device)
+    if token_scale_out is None:
+        token_scale_out = torch.empty(M, dtype=torch.float32, device=device)
+    _dev(out, torch.int8, "out")
+    _dev(token_scale_out, torch.float32, "token_scale_out")
+    if token_scale_out.numel() < M:
+        raise FptqError(-3, f"token_scale_out: {token_scale_out.numel()} values, need {M}")
+    return out, token_scale_out
+
+
+def fptq_norm_quantize8(x, residual=None, gain=None, scale_mode=SCALE_RMS, eps=0.0, out=None, token_scale_out=None, residual_out=None, want_residual=True):
+    """z = x + residual (bf16 [M, K], the residual optional), u = z * gain (bf16 [K], optional), to 8 bits: returns (codes int8 in the library's layout, fp32 [M]
+    scales with the RMS norm's factor of z in them, or without it for SCALE_NONE, bf16 [M, K] z or None).  residual_out may be x or the residual."""
+    done = None if _native is None else _native.norm_quantize8(x, residual, gain, scale_mode, eps, out, token_scale_out, residual_out, want_residual)
+    if done is not None:
+        return done
+    _dev(x, torch.bfloat16, "x")
+    if x.dim() != 2:
+        raise FptqError(-2, f"x: {tuple(x.shape)}, need [M, K]")
+    M, K = x.shape
+    if gain is not None and _dev(gain, torch.bfloat16, "gain").numel() != K:
+        raise FptqError(-2, f"gain: {gain.numel()} values, rows have {K}")
+    if residual is not None:
+        if _dev(residual, torch.bfloat16, "residual").shape != x.shape:
+            raise FptqError(-2, f"residual: {tuple(residual.shape)} does not go with x's {tuple(x.shape)}")
+        if residual_out is None and want_residual:
+            residual_out = torch.empty_like(x)
+    if residual_out is not None and _dev(residual_out, torch.bfloat16, "residual_out").shape != x.shape:
+        raise FptqError(-2, f"residual_out: {tuple(residual_out.shape)} does not go with x's {tuple(x.shape)}")
+    out, token_scale_out = _codes8(M, K, out, token_scale_out, x.device)
+    _check(lib().fptq_norm_quantize8(_ptr(x), _ptr(residual), _ptr(gain), M, K, int(scale_mode), float(eps), _ptr(out), out.numel(), _ptr(token_scale_out),
+                                     _ptr(residual_out), _stream()))
+    return out, token_scale_out, residual_out
+
+
+def fptq_gated_quantize8(gate, up, out=None, token_scale_out=None):
+    """silu(gate) * up to 8 bits: gate and up are bf16 [M, K] with any distance between rows (the halves of one projection's rows, for instance).  Returns (codes int8 in
+    the library's layout, fp32 [M] scales)."""
+    done = None if _native is None else _native.gated_quantize8(gate, up, out, token_scale_out)
+    if done is not None:
+        return done
+    for t, name in ((gate, "gate"), (up, "up")):
+        if not (t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1)):
+            raise TypeError(f"{name}: need a bf16 device tensor [M, K] whose last dimension is contiguous")
+    if gate.shape != up.shape:
+        raise FptqError(-2, f"up: {tuple(up.shape)} does not go with gate's {tuple(gate.shape)}")
+    M, K = gate.shape
+    out, token_scale_out = _codes8(M, K, out, token_scale_out, gate.device)
+    _check(lib().fptq_gated_quantize8(_ptr(gate), _ptr(up), M, K, gate.stride(0), up.stride(0), _ptr(out), out.numel(), _ptr(token_scale_out), _stream()))
+    return out, token_scale_out
+
+
+def fptq_w4a8_linear(xq8, token_scale, wq, M, N, K, group, w_scales, out=None, out_dtype=torch.bfloat16):
+    """Codes of 8 bits (from one of the quantizers above) x packed 4-bit weights with fp32 [ceil(K / group), N] scales: [M, N] in bf16 or fp32."""
+    if out_dtype is not torch.bfloat16 and out_dtype is not torch.float32:
+        raise TypeError(f"out_dtype: bf16 or fp32, not {out_dtype}")
+    done = None if _native is None else _native.w4a8_linear(xq8, token_scale, wq, M, N, K, group, w_scales, out, out_dtype is torch.float32)
+    if done is not None:
+        return done
+    _dev(xq8, torch.int8, "xq8")
+    _dev(token_scale, torch.float32, "token_scale")
+    _dev(wq, torch.uint8, "wq")
+    _dev(w_scales, torch.float32, "w_scales")
+    if group < 1:
+        raise FptqError(-2, f"group must be 32, 64 or a multiple of 128 (got {group})")
+    if xq8.numel() < _need8(M, K) or token_scale.numel() < M or wq.numel() < _need(N, K):
+        raise FptqError(-3, "codes, token_scale or packed weights smaller than the shape needs")
+    if w_scales.numel() < -(-K // group) * N:
+        raise FptqError(-3, f"w_scales: {w_scales.numel()} values, need {-(-K // group)} x {N}")
+    if out is None:
+        out = torch.empty((M, N), dtype=out_dtype, device=xq8.device)
+    elif _dev(out, out_dtype, "out").numel() < M * N:
+        raise FptqError(-3, f"out: {out.numel()} values, need {M} x {N}")
+    _check(lib().fptq_w4a8_linear(_ptr(xq8), _ptr(token_scale), _ptr(wq), M, N, K, group, _ptr(w_scales), _ptr(out), int(out_dtype == torch.float32), _stream()))
+    return out
+
+
+def fptq_unpack8(packed8, rows, K):
+    """Codes of 8 bits in the library's layout -> int8 [rows, K]."""
+    _dev(packed8, torch.int8, "packed8")
+    if packed8.numel() < fptq_packed8_bytes(rows, K):
+        raise FptqError(-3, "packed8 buffer smaller than the shape needs")
+    out = torch.empty((rows, K), dtype=torch.int8, device=packed8.device)
+    _check(lib().fptq_unpack8(_ptr(packed8), rows, K, _ptr(out), _stream()))
     return out
 
 

@@ -11,7 +11,7 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(CSRC, "libfptq.so")
 PROBE_LIB = os.path.join(CSRC, "libfptq_probe.so")
 SOURCES = ["fptq_api.hip", "fptq_pack.hip", "fptq_quant.hip", "fptq_gemm.hip", "fptq_prefill.hip", "fptq_gemv.hip", "fptq_hadamard.hip", "fptq_residual.hip",
-           "fptq_cache.hip", "fptq_decode_attention.hip", "fptq_prompt_attention.hip"]
+           "fptq_quant8.hip", "fptq_grouped.hip", "fptq_cache.hip", "fptq_decode_attention.hip", "fptq_prompt_attention.hip"]
 PROBE_SOURCES = ["fptq_probe.hip"]
 NATIVE_SOURCE, NATIVE = "fptq_native.cpp", os.path.join(HERE, "_native.so")      # the binding's fast path: host code, torch's C++ API
 

@@ -71,6 +71,9 @@ int device_cus_or_default()
     return info->cus;
 }
 
+// Tokens or channels of a call of 8-bit activations: rows of y stay below 2^31 bytes, and a launch below 2^32 threads.
+static const int64_t GROUPED_MOST = (int64_t)1 << 24;
+
 static int check_dims(const char *fn, int64_t a, int64_t b, const char *an, const char *bn)
 {
     if (a < 1 || b < 1 || a > MAX_ELEMS / b) {
@@ -670,6 +673,117 @@ int fptq_unpack(const void *packed, int64_t rows, int64_t K, int8_t *out_int8, v
     if ((rc = check_align("fptq_unpack", packed, 16, "packed"))) return rc;
     hipError_t e = launch_unpack((const uint8_t *)packed, rows, K, out_int8, (hipStream_t)stream);
     return e == hipSuccess ? FPTQ_OK : hip_fail("fptq_unpack", e);
+}
+
+// ---- 8-bit activations, weights in groups
+
+int64_t fptq_packed8_bytes(int64_t rows, int64_t K)
+{
+    const int rc = check_dims("fptq_packed8_bytes", rows, K, "rows", "K");
+    return rc ? rc : packed8_bytes(rows, K);
+}
+
+// what the two quantizers check of their outputs
+static int check_codes8(const char *fn, int64_t M, int64_t K, const void *xq8, int64_t xq8_bytes, const float *token_scale)
+{
+    int rc;
+    if ((rc = check_dims(fn, M, K, "M", "K"))) return rc;
+    if (xq8_bytes < packed8_bytes(M, K)) {
+        set_error("%s: xq8 buffer %lld bytes, need %lld", fn, (long long)xq8_bytes, (long long)packed8_bytes(M, K));
+        return FPTQ_ERR_SIZE;
+    }
+    if ((rc = check_align(fn, xq8, 16, "xq8"))) return rc;
+    return check_align(fn, token_scale, 4, "token_scale");
+}
+
+int fptq_norm_quantize8(const void *x_bf16, const void *residual, const void *gain, int64_t M, int64_t K, int scale_mode, float eps, void *xq8,
+                        int64_t xq8_bytes, float *token_scale, void *residual_out, void *stream)
+{
+    const char *fn = "fptq_norm_quantize8";
+    if (!x_bf16 || !xq8 || !token_scale) {
+        set_error("%s: NULL pointer", fn);
+        return FPTQ_ERR_NULL;
+    }
+    int rc;
+    if ((rc = check_codes8(fn, M, K, xq8, xq8_bytes, token_scale))) return rc;
+    if (scale_mode != FPTQ_SCALE_NONE && scale_mode != FPTQ_SCALE_RMS) {
+        set_error("%s: scale_mode must be FPTQ_SCALE_NONE or FPTQ_SCALE_RMS (got %d)", fn, scale_mode);
+        return FPTQ_ERR_MODE;
+    }
+    if (residual_out && !residual) {
+        set_error("%s: residual_out needs residual", fn);
+        return FPTQ_ERR_MODE;
+    }
+    if (!(eps >= 0.0f) || !std::isfinite(eps)) {
+        set_error("%s: eps must be finite and >= 0", fn);
+        return FPTQ_ERR_VALUE;
+    }
+    if ((rc = check_align(fn, x_bf16, 2, "x_bf16")) || (rc = check_align(fn, residual, 2, "residual")) || (rc = check_align(fn, gain, 2, "gain")) ||
+        (rc = check_align(fn, residual_out, 2, "residual_out")))
+        return rc;
+    return launched(fn, launch_norm_quantize8((const uint16_t *)x_bf16, (const uint16_t *)residual, (const uint16_t *)gain, M, K, scale_mode == FPTQ_SCALE_RMS,
+                                              eps, (uint8_t *)xq8, token_scale, (uint16_t *)residual_out, (hipStream_t)stream));
+}
+
+int fptq_gated_quantize8(const void *gate, const void *up, int64_t M, int64_t K, int64_t gate_stride, int64_t up_stride, void *xq8, int64_t xq8_bytes,
+                         float *token_scale, void *stream)
+{
+    const char *fn = "fptq_gated_quantize8";
+    if (!gate || !up || !xq8 || !token_scale) {
+        set_error("%s: NULL pointer", fn);
+        return FPTQ_ERR_NULL;
+    }
+    int rc;
+    if ((rc = check_codes8(fn, M, K, xq8, xq8_bytes, token_scale))) return rc;
+    if (M > 1 && (gate_stride < K || up_stride < K || gate_stride > MAX_ELEMS / M || up_stride > MAX_ELEMS / M)) {
+        set_error("%s: strides %lld and %lld do not go with rows of %lld values", fn, (long long)gate_stride, (long long)up_stride, (long long)K);
+        return FPTQ_ERR_SHAPE;
+    }
+    if ((rc = check_align(fn, gate, 2, "gate")) || (rc = check_align(fn, up, 2, "up"))) return rc;
+    return launched(fn, launch_gated_quantize8((const uint16_t *)gate, (const uint16_t *)up, M, K, M > 1 ? gate_stride : 0, M > 1 ? up_stride : 0, (uint8_t *)xq8,
+                                               token_scale, (hipStream_t)stream));
+}
+
+int fptq_w4a8_linear(const void *xq8, const float *token_scale, const void *w_packed, int64_t M, int64_t N, int64_t K, int64_t group,
+                     const float *w_scales, void *y, int y_type, void *stream)
+{
+    const char *fn = "fptq_w4a8_linear";
+    if (!xq8 || !token_scale || !w_packed || !w_scales || !y) {
+        set_error("%s: NULL pointer", fn);
+        return FPTQ_ERR_NULL;
+    }
+    int rc;
+    if ((rc = check_dims(fn, M, K, "M", "K")) || (rc = check_dims(fn, N, K, "N", "K")) || (rc = check_dims(fn, M, N, "M", "N"))) return rc;
+    if (group != 32 && group != 64 && (group < 128 || group % 128)) {
+        set_error("%s: group must be 32, 64 or a multiple of 128 (got %lld)", fn, (long long)group);
+        return FPTQ_ERR_SHAPE;
+    }
+    if (M > GROUPED_MOST || N > GROUPED_MOST || K > MAX_K) {
+        set_error("%s: M=%lld and N=%lld must be at most %lld, K=%lld at most %lld", fn, (long long)M, (long long)N, (long long)GROUPED_MOST, (long long)K,
+                  (long long)MAX_K);
+        return FPTQ_ERR_SHAPE;
+    }
+    if (y_type != FPTQ_BF16 && y_type != FPTQ_F32) {
+        set_error("%s: y_type must be FPTQ_BF16 or FPTQ_F32 (got %d)", fn, y_type);
+        return FPTQ_ERR_MODE;
+    }
+    if ((rc = check_align(fn, xq8, 16, "xq8")) || (rc = check_align(fn, w_packed, 16, "w_packed")) || (rc = check_align(fn, y, 16, "y")) ||
+        (rc = check_align(fn, token_scale, 4, "token_scale")) || (rc = check_align(fn, w_scales, 4, "w_scales")))
+        return rc;
+    return launched(fn, launch_grouped_linear((const uint8_t *)xq8, token_scale, (const uint8_t *)w_packed, M, N, K, group, w_scales, y, y_type,
+                                              (hipStream_t)stream));
+}
+
+int fptq_unpack8(const void *packed8, int64_t rows, int64_t K, int8_t *out_int8, void *stream)
+{
+    const char *fn = "fptq_unpack8";
+    if (!packed8 || !out_int8) {
+        set_error("%s: NULL pointer", fn);
+        return FPTQ_ERR_NULL;
+    }
+    int rc;
+    if ((rc = check_dims(fn, rows, K, "rows", "K")) || (rc = check_align(fn, packed8, 16, "packed8"))) return rc;
+    return launched(fn, launch_unpack8((const uint8_t *)packed8, rows, K, out_int8, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -19,6 +19,8 @@ constexpr int SEG = KT / 2;      // bytes per (row, tile) segment
 
 __host__ __device__ inline int64_t k_tiles(int64_t K) { return (K + KT - 1) / KT; }
 __host__ __device__ inline int64_t packed_bytes(int64_t rows, int64_t K) { return k_tiles(K) * rows * SEG; }
+// Codes of 8 bits: the same tiles with KT bytes a row, of every eight values the even ones first (the order that nibbles take when they are widened).
+__host__ __device__ inline int64_t packed8_bytes(int64_t rows, int64_t K) { return k_tiles(K) * rows * KT; }
 
 // error text of the calling thread (set by the API layer)
 void set_error(const char *fmt, ...);
@@ -53,6 +55,13 @@ int prefill_tile(int64_t M, int64_t N, int64_t K);      // tokens per tile (256,
 hipError_t launch_linear_decode(const uint8_t *xq, const uint8_t *wq, int64_t M, int64_t N, int64_t K, float s_a,
                                 const float *s_w, const float *d, int zp, const int32_t *wsum, uint16_t *y, int32_t *acc,
                                 hipStream_t s);
+hipError_t launch_norm_quantize8(const uint16_t *x, const uint16_t *residual, const uint16_t *gain, int64_t M, int64_t K, int rms, float eps, uint8_t *out,
+                                 float *scale, uint16_t *residual_out, hipStream_t s);
+hipError_t launch_gated_quantize8(const uint16_t *gate, const uint16_t *up, int64_t M, int64_t K, int64_t gate_stride, int64_t up_stride, uint8_t *out,
+                                  float *scale, hipStream_t s);
+hipError_t launch_unpack8(const uint8_t *packed, int64_t rows, int64_t K, int8_t *out, hipStream_t s);
+hipError_t launch_grouped_linear(const uint8_t *x, const float *token_scale, const uint8_t *w, int64_t M, int64_t N, int64_t K, int64_t group,
+                                 const float *scales, void *y, int y_type, hipStream_t s);
 
 void set_gemm_tile(int tile);
 void set_gemm_map(int mode);

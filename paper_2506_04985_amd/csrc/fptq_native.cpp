@@ -454,10 +454,94 @@ PyObject *prompt_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+int64_t need8(int64_t rows, int64_t K) { return (K + 127) / 128 * rows * 128; }
+
+// a caller's output of the given type and at least n values, or a new one
+Output checked(PyObject *o, std::initializer_list<int64_t> sizes, at::ScalarType type, const at::Tensor &like)
+{
+    int64_t n = 1;
+    for (int64_t s : sizes) n *= s;
+    if (o != Py_None && input(o, type).numel() < n) throw Slow();
+    return Output(o, sizes, type, like);
+}
+
+// (x, residual, gain, scale_mode, eps, out, token_scale_out, residual_out, want_residual)
+PyObject *norm_quantize8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 9, [&]() -> PyObject * {
+        const at::Tensor &x = input(a[0], at::kBFloat16);
+        int64_t M, K;
+        matrix(x, M, K);
+        const void *residual = nullptr, *gain = nullptr;
+        if (a[1] != Py_None) {
+            const at::Tensor &r = input(a[1], at::kBFloat16);
+            if (r.sizes() != x.sizes()) throw Slow();
+            residual = r.data_ptr();
+        }
+        if (a[2] != Py_None) {
+            const at::Tensor &g = input(a[2], at::kBFloat16);
+            if (g.numel() != K) throw Slow();
+            gain = g.data_ptr();
+        }
+        const int mode = (int)integer(a[3]);
+        const float eps = number(a[4]);
+        Output out = checked(a[5], {need8(M, K)}, at::kChar, x), s = checked(a[6], {M}, at::kFloat, x), sum;
+        if (a[7] != Py_None) {
+            if (!residual || input(a[7], at::kBFloat16).sizes() != x.sizes()) throw Slow();
+            sum = Output(a[7], {M, K}, at::kBFloat16, x);
+        } else if (truth(a[8]) && residual) {
+            sum = Output(Py_None, {M, K}, at::kBFloat16, x);
+        }
+        void *const st = where().stream;
+        launch({&out, &s, &sum}, [&] {
+            return fptq_norm_quantize8(x.data_ptr(), residual, gain, M, K, mode, eps, out.ptr, out.numel, (float *)s.ptr, sum.ptr, st);
+        });
+        return tuple({&out, &s, &sum});
+    });
+}
+
+// (gate, up, out, token_scale_out)
+PyObject *gated_quantize8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 4, [&]() -> PyObject * {
+        const at::Tensor &gate = device_tensor(a[0]), &up = device_tensor(a[1]);
+        int64_t M, K;
+        matrix(gate, M, K);
+        if (gate.scalar_type() != at::kBFloat16 || up.scalar_type() != at::kBFloat16 || up.sizes() != gate.sizes()) throw Slow();
+        if (K > 1 && (gate.stride(1) != 1 || up.stride(1) != 1)) throw Slow();
+        const int64_t gate_stride = gate.stride(0), up_stride = up.stride(0);
+        Output out = checked(a[2], {need8(M, K)}, at::kChar, gate), s = checked(a[3], {M}, at::kFloat, gate);
+        void *const st = where().stream;
+        launch({&out, &s}, [&] {
+            return fptq_gated_quantize8(gate.data_ptr(), up.data_ptr(), M, K, gate_stride, up_stride, out.ptr, out.numel, (float *)s.ptr, st);
+        });
+        return tuple({&out, &s});
+    });
+}
+
+// (xq8, token_scale, wq, M, N, K, group, w_scales, out, fp32)
+PyObject *w4a8_linear(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 10, [&]() -> PyObject * {
+        const at::Tensor &xq = input(a[0], at::kChar), &s = input(a[1], at::kFloat), &wq = input(a[2], at::kByte), &w_scales = input(a[7], at::kFloat);
+        const int64_t M = integer(a[3]), N = integer(a[4]), K = integer(a[5]), group = integer(a[6]);
+        if (M < 1 || N < 1 || K < 1 || group < 1 || M > (1ll << 40) / K || N > (1ll << 40) / K || M > (1ll << 40) / N) throw Slow();
+        if (xq.numel() < need8(M, K) || s.numel() < M || wq.numel() < need(N, K) || w_scales.numel() < ((K - 1) / group + 1) * N) throw Slow();
+        const bool fp32 = truth(a[9]);
+        Output y = checked(a[8], {M, N}, fp32 ? at::kFloat : at::kBFloat16, xq);
+        void *const st = where().stream;
+        launch({&y}, [&] {
+            return fptq_w4a8_linear(xq.data_ptr(), (const float *)s.data_ptr(), wq.data_ptr(), M, N, K, group, (const float *)w_scales.data_ptr(), y.ptr,
+                                    fp32 ? FPTQ_F32 : FPTQ_BF16, st);
+        });
+        return y.take();
+    });
+}
+
 #define FPTQ_FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FPTQ_FAST(pack_weights), FPTQ_FAST(weight_row_sums), FPTQ_FAST(quantize_act), FPTQ_FAST(quantize_act_dynamic),
                          FPTQ_FAST(residual_norm_quantize), FPTQ_FAST(linear), FPTQ_FAST(cache_append), FPTQ_FAST(cached_attention),
-                         FPTQ_FAST(prompt_attention), {nullptr, nullptr, 0, nullptr}};
+                         FPTQ_FAST(prompt_attention), FPTQ_FAST(norm_quantize8), FPTQ_FAST(gated_quantize8), FPTQ_FAST(w4a8_linear), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

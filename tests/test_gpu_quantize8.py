@@ -1,0 +1,174 @@
+"""Quantizers to 8 bits on the GPU: codes, scales and the new residual are unique (fp32 recipe, fp64 sums), so they are compared bit by bit with the oracle's.
+
+The one exception is the RMS factor: its sum of squares is in fp64 in an order of the kernel's own, whose rounding can move the fp32 result by a step only where the exact
+value lies within 2^-40 of a tie; scales are therefore allowed one step, and it is counted."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import grouped
+from paper_2506_04985_amd import binding as fptq
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [(1, 1), (1, 7), (2, 8), (3, 9), (5, 127), (4, 128), (3, 129), (1, 2048), (2, 2056), (1, 4096), (7, 4100), (3, 4099), (1030, 63), (1030, 512), (1100, 515),
+          (1100, 1024), (1027, 1500), (1029, 2048), (2, 8192), (3, 8189), (2, 8200), (1, 16384), (2, 16390), (3, 16383), (2, 28672), (2, 32768), (1, 32761), (1, 32769), (2, 40960)]
+
+
+def host(t):
+    return t.detach().cpu().float().numpy()
+
+
+def rows(g, M, K, spread=True):
+    x = torch.randn((M, K), device="cuda", generator=g)
+    if spread:
+        x *= torch.exp(3.0 * torch.randn((M, 1), device="cuda", generator=g)) * (1 + 30.0 * (torch.rand((K,), device="cuda", generator=g) < 0.01))
+    return x.to(torch.bfloat16)
+
+
+def same_scales(got, want):
+    got, want = got.cpu().numpy(), np.asarray(want, np.float32)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    ok = ~np.isnan(want)
+    steps = np.abs(got[ok].view(np.int32).astype(np.int64) - want[ok].view(np.int32))
+    assert steps.size == 0 or (steps.max() <= 1 and (steps > 0).sum() <= 1)
+
+
+def guarded_codes(M, K, fill=77):
+    """An output with 64 bytes more on either side, which have to stay as they are."""
+    n = fptq.fptq_packed8_bytes(M, K)
+    whole = torch.full((n + 128,), fill, dtype=torch.int8, device="cuda")
+    return whole, whole[64:64 + n]
+
+
+def untouched(whole, fill=77):
+    return bool((whole[:64] == fill).all()) and bool((whole[-64:] == fill).all())
+
+
+@pytest.mark.parametrize("M,K", SHAPES)
+@pytest.mark.parametrize("residual,gain,rms", [(True, True, True), (False, False, False), (True, False, False), (False, True, True)])
+def test_norm(M, K, residual, gain, rms):
+    g = torch.Generator(device="cuda").manual_seed(M * 100003 + K)
+    x = rows(g, M, K)
+    r = rows(g, M, K, False) if residual else None
+    w = (1 + 0.5 * torch.randn((K,), device="cuda", generator=g)).to(torch.bfloat16) if gain else None
+    whole, out = guarded_codes(M, K)
+    codes, scale, z = fptq.fptq_norm_quantize8(x, r, w, fptq.SCALE_RMS if rms else fptq.SCALE_NONE, 1e-5, out=out)
+    want_z, u, inv = grouped.residual_norm(host(x), None if r is None else host(r), None if w is None else host(w), 1e-5 if rms else None)
+    want, want_scale = grouped.quantize_rows(u, inv)
+    assert codes.data_ptr() == out.data_ptr() and untouched(whole)
+    assert np.array_equal(codes.cpu().numpy(), grouped.lay_out(want))
+    assert np.array_equal(fptq.fptq_unpack8(codes, M, K).cpu().numpy(), want)
+    same_scales(scale, want_scale)
+    if residual:
+        assert torch.equal(z.cpu(), torch.from_numpy(want_z).to(torch.bfloat16))
+    else:
+        assert z is None
+
+
+@pytest.mark.parametrize("M,K", SHAPES)
+def test_gated(M, K):
+    g = torch.Generator(device="cuda").manual_seed(M * 7 + K)
+    both = rows(g, M, 2 * K)
+    gate, up = both.split(K, 1)
+    whole, out = guarded_codes(M, K)
+    codes, scale = fptq.fptq_gated_quantize8(gate, up, out=out)
+    want, want_scale = grouped.quantize_rows(grouped.gated(host(gate), host(up)))
+    assert untouched(whole)
+    assert np.array_equal(codes.cpu().numpy(), grouped.lay_out(want))
+    assert np.array_equal(scale.cpu().numpy(), want_scale)
+
+
+def test_silu_of_every_bf16_value():
+    """With up = 1 and one value a row (and a second one, 0) the scale is |silu(g)| / 127: every finite bf16, compared bit by bit through two roundings that cannot differ."""
+    bits = torch.arange(65536, dtype=torch.int32, device="cuda").to(torch.int16)
+    gate = torch.zeros((65536, 2), dtype=torch.bfloat16, device="cuda")
+    gate[:, 0] = bits.view(torch.bfloat16)
+    up = torch.ones_like(gate)
+    codes, scale = fptq.fptq_gated_quantize8(gate, up)
+    want, want_scale = grouped.quantize_rows(grouped.gated(host(gate), host(up)))
+    assert np.array_equal(scale.cpu().numpy(), want_scale, equal_nan=True)
+    assert np.array_equal(codes.cpu().numpy(), grouped.lay_out(want))
+    assert int(torch.isnan(scale).sum()) == 2 + 2 * 127                 # the infinities and the NaN
+
+
+@pytest.mark.parametrize("M,K", [(9, 40), (1025, 40), (5, 4096), (3, 5000), (2, 20000), (2, 33000)])
+def test_rows_of_zeros_of_tiny_values_and_with_values_that_are_not_finite(M, K):
+    g = torch.Generator(device="cuda").manual_seed(K)
+    x = rows(g, M, K)
+    x[0] = 0
+    x[1] = 2.0 ** -126
+    if M > 2:
+        x[2, K - 1] = float("inf")
+    if M > 3:
+        x[3, K // 2], x[4, 0] = float("nan"), float("-inf")
+    for eps in (0.0, 1e-5):
+        codes, scale, _ = fptq.fptq_norm_quantize8(x, eps=eps)
+        z, u, inv = grouped.residual_norm(host(x), None, None, max(eps, 1e-30))           # a row of zeros has scale 0 whatever its factor
+        want, want_scale = grouped.quantize_rows(u, inv)
+        assert np.array_equal(fptq.fptq_unpack8(codes, M, K).cpu().numpy(), want)
+        if eps:
+            same_scales(scale, want_scale)
+        assert float(scale[0]) == 0.0 and not bool(torch.isnan(scale[1]))
+    gate = torch.full_like(x, 20.0)                                          # silu(20) = 20 to the last bit of fp32 but one
+    codes, scale = fptq.fptq_gated_quantize8(gate, x)
+    want, want_scale = grouped.quantize_rows(grouped.gated(host(gate), host(x)))
+    assert np.array_equal(fptq.fptq_unpack8(codes, M, K).cpu().numpy(), want)
+    assert np.array_equal(scale.cpu().numpy(), want_scale, equal_nan=True)
+
+
+def test_a_sum_and_a_product_beyond_fp32_count_as_not_finite():
+    x = torch.full((2, 16), 3.0e38, dtype=torch.bfloat16, device="cuda")
+    codes, scale, z = fptq.fptq_norm_quantize8(x, x, None, fptq.SCALE_NONE)
+    assert bool(torch.isnan(scale).all()) and not bool(codes.any()) and bool(torch.isinf(z).all())
+    codes, scale = fptq.fptq_gated_quantize8(x, x)
+    assert bool(torch.isnan(scale).all()) and not bool(codes.any())
+
+
+@pytest.mark.parametrize("M,K", [(3, 64), (2, 4096), (1500, 100), (1500, 2048), (4, 4099), (2, 16385), (1, 33001)])
+@pytest.mark.parametrize("onto", ["x", "residual"])
+def test_the_new_residual_in_place(M, K, onto):
+    g = torch.Generator(device="cuda").manual_seed(K)
+    x, r = rows(g, M, K), rows(g, M, K)
+    w = torch.rand((K,), device="cuda", generator=g).to(torch.bfloat16)
+    apart = fptq.fptq_norm_quantize8(x, r, w, eps=1e-6)
+    a, b = x.clone(), r.clone()
+    same = fptq.fptq_norm_quantize8(a, b, w, eps=1e-6, residual_out=a if onto == "x" else b)
+    assert all(torch.equal(p, q) for p, q in zip(apart, same))
+    assert torch.equal(b if onto == "x" else a, r if onto == "x" else x)
+    none = fptq.fptq_norm_quantize8(x, r, w, eps=1e-6, want_residual=False)
+    assert none[2] is None and torch.equal(none[0], apart[0]) and torch.equal(none[1], apart[1])
+
+
+@pytest.mark.parametrize("K", [64, 1000, 4096, 9001])
+@pytest.mark.parametrize("shift", [1, 3, 8])
+def test_any_alignment_and_any_distance_between_rows(K, shift):
+    g = torch.Generator(device="cuda").manual_seed(K + shift)
+    M = 5
+    flat = rows(g, 1, M * K + 16, False).view(-1)
+    x = flat[shift:shift + M * K].view(M, K)
+    w = rows(g, 1, K + 16, False).view(-1)[shift:shift + K]
+    out = torch.zeros(M * K + 16, dtype=torch.bfloat16, device="cuda")
+    z = out[shift:shift + M * K].view(M, K)
+    got = fptq.fptq_norm_quantize8(x, x, w, eps=1e-5, residual_out=z)
+    want = fptq.fptq_norm_quantize8(x.clone(), x.clone(), w.clone(), eps=1e-5)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert not bool(out[:shift].any()) and not bool(out[shift + M * K:].any())
+    wide = rows(g, M, 3 * K + 24)
+    gate, up = wide[:, shift:shift + K], wide[:, K + 11:2 * K + 11]
+    got, want = fptq.fptq_gated_quantize8(gate, up), fptq.fptq_gated_quantize8(gate.contiguous(), up.contiguous())
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_more_rows_than_one_launch_takes():
+    """A launch has 2^20 workgroups at most; they go on from row to row."""
+    for M, K in ((4 * (1 << 20) + 5, 8), ((1 << 20) + 3, 72)):
+        g = torch.Generator(device="cuda").manual_seed(K)
+        x = torch.randn((M, K), device="cuda", generator=g).to(torch.bfloat16)
+        codes, scale, _ = fptq.fptq_norm_quantize8(x, scale_mode=fptq.SCALE_NONE)
+        at = torch.tensor([0, 1, (1 << 20) - 1, 1 << 20, M - 2, M - 1])
+        want, want_scale = grouped.quantize_rows(host(x[at.cuda()]))
+        assert np.array_equal(codes.view(1, M, 16, 8)[0][at.cuda()].cpu().numpy().reshape(-1), grouped.lay_out(want))
+        assert np.array_equal(scale[at.cuda()].cpu().numpy(), want_scale)
+        del x, codes
+        torch.cuda.empty_cache()

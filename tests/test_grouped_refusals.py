@@ -1,0 +1,58 @@
+"""What the calls of 8-bit activations refuse: before any launch, so no GPU is needed."""
+import ctypes
+
+import pytest
+
+from paper_2506_04985_amd import binding as fptq
+
+P = ctypes.c_void_p(1 << 20)
+ODD = ctypes.c_void_p((1 << 20) + 1)
+TWO = ctypes.c_void_p((1 << 20) + 2)
+EIGHT = ctypes.c_void_p((1 << 20) + 8)
+NULL, SHAPE, SIZE, MODE, VALUE, ALIGN = -1, -2, -3, -4, -6, -7
+
+
+def refused(name, arguments, order, code, **changed):
+    L = fptq.lib()
+    assert not set(changed) - set(order)
+    assert getattr(L, name)(*[changed.get(k, arguments[k]) for k in order]) == code, (name, changed)
+    assert name.encode() in L.fptq_last_error()
+
+
+NORM = dict(x=P, residual=P, gain=P, M=4, K=300, mode=1, eps=1e-5, out=P, nbytes=4 * 384, scale=P, z=P, stream=None)
+GATED = dict(gate=P, up=P, M=4, K=300, gs=600, us=600, out=P, nbytes=4 * 384, scale=P, stream=None)
+LINEAR = dict(x=P, s=P, w=P, M=4, N=5, K=300, group=64, ws=P, y=P, type=0, stream=None)
+
+
+@pytest.mark.parametrize("code,changed", [
+    (NULL, dict(x=None)), (NULL, dict(out=None)), (NULL, dict(scale=None)), (SHAPE, dict(M=0)), (SHAPE, dict(K=0)), (SHAPE, dict(M=-1)), (SHAPE, dict(M=1 << 40)),
+    (SIZE, dict(nbytes=4 * 384 - 1)), (SIZE, dict(nbytes=0)), (MODE, dict(mode=2)), (MODE, dict(mode=-1)), (MODE, dict(residual=None)),
+    (VALUE, dict(eps=-1e-9)), (VALUE, dict(eps=float("nan"))), (VALUE, dict(eps=float("inf"))),
+    (ALIGN, dict(x=ODD)), (ALIGN, dict(residual=ODD)), (ALIGN, dict(gain=ODD)), (ALIGN, dict(z=ODD)), (ALIGN, dict(out=EIGHT)), (ALIGN, dict(scale=TWO))])
+def test_norm(code, changed):
+    refused("fptq_norm_quantize8", NORM, list(NORM), code, **changed)
+
+
+@pytest.mark.parametrize("code,changed", [
+    (NULL, dict(gate=None)), (NULL, dict(up=None)), (NULL, dict(out=None)), (NULL, dict(scale=None)), (SHAPE, dict(M=0)), (SHAPE, dict(K=-3)),
+    (SHAPE, dict(gs=299)), (SHAPE, dict(us=299)), (SHAPE, dict(us=-600)), (SHAPE, dict(gs=1 << 39)), (SIZE, dict(nbytes=1535)),
+    (ALIGN, dict(gate=ODD)), (ALIGN, dict(up=ODD)), (ALIGN, dict(out=EIGHT)), (ALIGN, dict(scale=TWO))])
+def test_gated(code, changed):
+    refused("fptq_gated_quantize8", GATED, list(GATED), code, **changed)
+
+
+@pytest.mark.parametrize("code,changed", [
+    (NULL, dict(x=None)), (NULL, dict(s=None)), (NULL, dict(w=None)), (NULL, dict(ws=None)), (NULL, dict(y=None)),
+    (SHAPE, dict(M=0)), (SHAPE, dict(N=0)), (SHAPE, dict(K=0)), (SHAPE, dict(M=1 << 25)), (SHAPE, dict(N=(1 << 24) + 1)), (SHAPE, dict(K=1 << 25)),
+    (SHAPE, dict(group=0)), (SHAPE, dict(group=-128)), (SHAPE, dict(group=16)), (SHAPE, dict(group=96)), (SHAPE, dict(group=130)), (SHAPE, dict(group=192)),
+    (MODE, dict(type=2)), (MODE, dict(type=-1)), (ALIGN, dict(x=EIGHT)), (ALIGN, dict(w=EIGHT)), (ALIGN, dict(y=EIGHT)), (ALIGN, dict(s=TWO)), (ALIGN, dict(ws=TWO))])
+def test_linear(code, changed):
+    refused("fptq_w4a8_linear", LINEAR, list(LINEAR), code, **changed)
+
+
+def test_sizes_and_unpack():
+    L = fptq.lib()
+    assert L.fptq_packed8_bytes(1, 1) == 128 and L.fptq_packed8_bytes(10, 129) == 2560 and L.fptq_packed8_bytes(8192, 28672) == 8192 * 28672
+    assert L.fptq_packed8_bytes(0, 1) == SHAPE and L.fptq_packed8_bytes(1, -1) == SHAPE
+    assert L.fptq_unpack8(None, 1, 1, P, None) == NULL and L.fptq_unpack8(P, 1, 1, None, None) == NULL
+    assert L.fptq_unpack8(P, 0, 1, P, None) == SHAPE and L.fptq_unpack8(EIGHT, 1, 1, P, None) == ALIGN
