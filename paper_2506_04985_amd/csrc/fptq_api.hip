@@ -53,6 +53,7 @@ hipError_t device_info(const DeviceInfo **out)
             info.cus = cus > 0 ? cus : DEFAULT_CUS;
             if ((e = gemm_device_init(&info)) != hipSuccess) return e;
             if ((e = prefill_device_init()) != hipSuccess) return e;
+            if ((e = grouped_device_init()) != hipSuccess) return e;
             g_devices[dev] = info;
             g_device_ready[dev].store(true, std::memory_order_release);
         }

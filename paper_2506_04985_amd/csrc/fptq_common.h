@@ -93,6 +93,7 @@ int device_cus_or_default();                     // compute units of the current
 // what each translation unit contributes to that set-up (called with the device current, under the set-up lock)
 hipError_t gemm_device_init(DeviceInfo *info);
 hipError_t prefill_device_init();
+hipError_t grouped_device_init();
 
 // ---- what several kernel sources share
 

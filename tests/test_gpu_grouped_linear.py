@@ -54,6 +54,15 @@ def test_products(M, N, K, group):
     check(run(*case, group, torch.bfloat16), y, mass, K, group)
 
 
+@pytest.mark.parametrize("group", [32, 64, 128, 256])
+@pytest.mark.parametrize("M,N,K", [(2600, 5200, 200), (3500, 3601, 100), (300, 26000, 129)])
+def test_products_of_many_tiles(M, N, K, group):
+    case = draw(M, N, K, group)
+    y, mass = grouped.linear(*case[:3], group, case[3])
+    check(run(*case, group), y, mass, K, group)
+    check(run(*case, group, torch.bfloat16), y, mass, K, group)
+
+
 @pytest.mark.parametrize("M", [1, 40, 300])
 def test_one_scale_a_channel(M):
     N, K = 96, 700
