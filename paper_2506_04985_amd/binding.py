@@ -25,7 +25,7 @@ EXPORTS = ["fptq_version", "fptq_last_error", "fptq_init", "fptq_packed_bytes", 
            "fptq_cache_append", "fptq_cached_attention_scratch_bytes", "fptq_cached_attention", "fptq_prompt_attention",
            "fptq_packed8_bytes", "fptq_norm_quantize8", "fptq_gated_quantize8", "fptq_w4a8_linear", "fptq_unpack8"]
 TESTING_EXPORTS = ["fptq_set_gemm_tile", "fptq_set_gemm_map", "fptq_set_decode_shape", "fptq_set_linear_prefill",
-                   "fptq_linear_launch_plan"]
+                   "fptq_linear_launch_plan", "fptq_set_grouped_kernel", "fptq_grouped_kernel"]
 
 _lib = None
 _native = None      # the native fast path (csrc/fptq_native.cpp), loaded with the library: a call returns None where it leaves the call to Python
@@ -116,6 +116,10 @@ def lib():
         L.fptq_gated_quantize8.argtypes = [p, p, i64, i64, i64, i64, p, i64, p, p]
         L.fptq_w4a8_linear.restype = i32
         L.fptq_w4a8_linear.argtypes = [p, p, p, i64, i64, i64, i64, p, p, i32, p]
+        L.fptq_set_grouped_kernel.restype = i32
+        L.fptq_set_grouped_kernel.argtypes = [i32]
+        L.fptq_grouped_kernel.restype = i32
+        L.fptq_grouped_kernel.argtypes = [i64, i64, i64, i64]
         L.fptq_unpack8.restype = i32
         L.fptq_unpack8.argtypes = [p, i64, i64, p, p]
         try:
@@ -635,6 +639,10 @@ def fptq_unpack8(packed8, rows, K):
     out = torch.empty((rows, K), dtype=torch.int8, device=packed8.device)
     _check(lib().fptq_unpack8(_ptr(packed8), rows, K, _ptr(out), _stream()))
     return out
+
+
+def fptq_set_grouped_kernel(kernel):
+    _check(lib().fptq_set_grouped_kernel(int(kernel)))
 
 
 def fptq_set_gemm_map(mode):

@@ -72,8 +72,8 @@ int device_cus_or_default()
     return info->cus;
 }
 
-// Tokens or channels of a call of 8-bit activations: rows of y stay below 2^31 bytes, and a launch below 2^32 threads.
-static const int64_t GROUPED_MOST = (int64_t)1 << 24;
+// Tokens or channels, and outputs, of a linear call with 8-bit activations: what keeps a launch below 2^32 threads.
+static const int64_t GROUPED_MOST = (int64_t)1 << 24, GROUPED_OUTPUTS = (int64_t)1 << 37;
 
 static int check_dims(const char *fn, int64_t a, int64_t b, const char *an, const char *bn)
 {
@@ -764,6 +764,10 @@ int fptq_w4a8_linear(const void *xq8, const float *token_scale, const void *w_pa
                   (long long)MAX_K);
         return FPTQ_ERR_SHAPE;
     }
+    if (M > GROUPED_OUTPUTS / N) {
+        set_error("%s: M=%lld and N=%lld make more than %lld outputs", fn, (long long)M, (long long)N, (long long)GROUPED_OUTPUTS);
+        return FPTQ_ERR_SHAPE;
+    }
     if (y_type != FPTQ_BF16 && y_type != FPTQ_F32) {
         set_error("%s: y_type must be FPTQ_BF16 or FPTQ_F32 (got %d)", fn, y_type);
         return FPTQ_ERR_MODE;
@@ -774,6 +778,17 @@ int fptq_w4a8_linear(const void *xq8, const float *token_scale, const void *w_pa
     return launched(fn, launch_grouped_linear((const uint8_t *)xq8, token_scale, (const uint8_t *)w_packed, M, N, K, group, w_scales, y, y_type,
                                               (hipStream_t)stream));
 }
+
+int fptq_set_grouped_kernel(int kernel)
+{
+    if (!set_grouped_kernel(kernel)) {
+        set_error("fptq_set_grouped_kernel: kernel must be 0..12");
+        return FPTQ_ERR_VALUE;
+    }
+    return FPTQ_OK;
+}
+
+int fptq_grouped_kernel(int64_t M, int64_t N, int64_t K, int64_t group) { return M < 1 || N < 1 || K < 1 || group < 1 ? FPTQ_ERR_SHAPE : 1 + grouped_kernel(M, N, K, group); }
 
 int fptq_unpack8(const void *packed8, int64_t rows, int64_t K, int8_t *out_int8, void *stream)
 {

@@ -5,6 +5,8 @@
 // Nibbles are widened to bytes that hold 16 * value as in the other linears, (p << 4) & 0xF0F0F0F0 and p & 0xF0F0F0F0, and the codes of eight k lie
 // in that order, so they are operands as they are.  Of 128 k or fewer, 16 * sum stays below 2^21 in magnitude, which fp32 holds exactly; the 1/16 goes into the
 // token's scale, exactly as well.  Groups of several K tiles take their scale once a tile.
+#include <utility>
+
 #include "fptq_common.h"
 
 namespace fptq {
@@ -40,117 +42,93 @@ __device__ inline void by_group(v4i &w)
     w = v4i{d0, d1, d2, d3};
 }
 
-// A workgroup owns 16 RT channels, its waves split K (wave w takes K tiles w, w + WAVES, ...), MT groups of 16 tokens.  Tokens are the rows of the MFMA's
-// result and channels its columns, so that a lane has one channel, and one scale of it a group.
-template <int WAVES, int U, int MT, int RT, int GT>
+// Few tokens.  A workgroup owns 16 RT channels of 16 tokens, its waves split K (wave w takes K tiles w, w + WAVES, ...) with one K tile in flight each and
+// several workgroups a CU.  Bound: HBM, the weights once, streamed.  Tokens are the rows of the MFMA's result and channels its columns, so that a lane has one channel, and
+// one scale of it a group.  The waves' fp32 sums meet in LDS and are added in order.
+template <int WAVES, int RT, int GT>
 __global__ __launch_bounds__(64 * WAVES) void grouped_few_kernel(const uint8_t *__restrict__ x, const uint8_t *__restrict__ w, const float *__restrict__ scales, int M,
                                                                  int N, int ktiles, int groups, uint32_t tiles_per_group, uint32_t reciprocal_of_it,
                                                                  const float *__restrict__ token_scale, void *__restrict__ y, int y_type)
 {
-    __shared__ float red[WAVES][RT * MT * 256];
+    __shared__ float red[WAVES][RT * 256];
+    static_assert(RT * 256 <= 64 * WAVES, "an output a thread");
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n0 = blockIdx.x * (16 * RT), m0 = blockIdx.y * (16 * MT);
+    const int n0 = blockIdx.x * (16 * RT), m0 = blockIdx.y * 16;
     const int64_t w_slab = (int64_t)N * SEG, x_slab = (int64_t)M * KT;
-    const uint8_t *wp[RT], *xp[MT];
+    const uint8_t *wp[RT];
     const float *sp[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const int n = min(n0 + rt * 16 + c, N - 1);
+        const int n = min(n0 + rt * 16 + c, N - 1);      // channels and tokens past the end repeat the last one; what they make is not stored
         wp[rt] = w + (int64_t)n * SEG + q * 16;
         sp[rt] = scales + n;
     }
     // a token's 16 or 8 codes for each MFMA, as by_group leaves the weights
-    constexpr int STEPS = GT == 4 ? 4 : 2;
+    constexpr int STEPS = GT == 4 ? 4 : 2, X_STEP = GT == 1 ? 16 : GT == 2 ? 64 : 32;
     const int x_first = GT == 1 ? q * 32 : GT == 2 ? (q & 1) * 32 + (q >> 1) * 16 : q * 8;
-    constexpr int x_step = GT == 1 ? 16 : GT == 2 ? 64 : 32;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) xp[mt] = x + (int64_t)min(m0 + mt * 16 + c, M - 1) * KT + x_first;
+    const uint8_t *const xp = x + (int64_t)min(m0 + c, M - 1) * KT + x_first;
+    // what the thread's output will need, fetched now: the kernel is too short to end on a memory latency
+    const int t_out = m0 + tid / (16 * RT), n_out = n0 + tid % (16 * RT);
+    const bool stores = tid < RT * 256 && t_out < M && n_out < N;
+    const float ts = stores ? token_scale[t_out] * 0.0625f : 0.0f;
 
-    v4f sum[RT][MT];
+    v4f sum[RT];
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
+    for (int rt = 0; rt < RT; ++rt) sum[rt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int kt = wave; kt < ktiles; kt += WAVES) {
+        v4i wv[RT], xv[STEPS];
+        float sv[RT][GT];
+        uint32_t first, rest;
+        divide((uint32_t)kt, tiles_per_group, reciprocal_of_it, first, rest);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) sum[rt][mt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    const int T = wave < ktiles ? (ktiles - wave + WAVES - 1) / WAVES : 0;
-    for (int base = 0; base < T; base += U) {
-        v4i wv[RT][U];
-        float sv[RT][U][GT];
+        for (int rt = 0; rt < RT; ++rt) {
+            wv[rt] = __builtin_nontemporal_load(reinterpret_cast<const v4i *>(wp[rt] + kt * w_slab));
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (base + u < T) {
-                const int64_t kt = wave + (base + u) * WAVES;
-                uint32_t first, rest;
-                divide((uint32_t)kt, tiles_per_group, reciprocal_of_it, first, rest);
+            for (int g = 0; g < GT; ++g) sv[rt][g] = sp[rt][(int64_t)min((int)first * GT + g, groups - 1) * N];      // a last tile may hold fewer groups: its weights there are zero
+        }
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    wv[rt][u] = __builtin_nontemporal_load(reinterpret_cast<const v4i *>(wp[rt] + kt * w_slab));
+        for (int j = 0; j < STEPS; ++j) {
+            if (GT == 4) {
+                const v2i v = *reinterpret_cast<const v2i *>(xp + kt * x_slab + j * X_STEP);
+                xv[j] = v4i{v.x, v.y, 0, 0};
+            } else {
+                xv[j] = *reinterpret_cast<const v4i *>(xp + kt * x_slab + j * X_STEP);
+            }
+        }
 #pragma unroll
-                    for (int g = 0; g < GT; ++g)      // a last tile may hold fewer groups: its weights there are zero
-                        sv[rt][u][g] = sp[rt][(int64_t)min((int)first * GT + g, groups - 1) * N];
+        for (int rt = 0; rt < RT; ++rt) {
+            by_group<GT>(wv[rt]);
+            v4i acc = {0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < STEPS; ++j) {
+                if constexpr (GT == 4)
+                    acc = __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, v2i{xv[j].x, xv[j].y}), __builtin_bit_cast(long, widen1(wv[rt][j])), v4i{0, 0, 0, 0}, 0, 0, 0);
+                else
+                    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(xv[j], widen2(wv[rt][2 * j], wv[rt][2 * j + 1]), GT == 2 ? v4i{0, 0, 0, 0} : acc, 0, 0, 0);
+                if (GT != 1 || j == 1) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sum[rt][r] = __builtin_fmaf((float)acc[r], sv[rt][GT == 1 ? 0 : j], sum[rt][r]);
                 }
             }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (base + u < T) {
-                const int64_t kt = wave + (base + u) * WAVES;
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    v4i xv[STEPS];
-#pragma unroll
-                    for (int j = 0; j < STEPS; ++j) {
-                        if (GT == 4) {
-                            const v2i v = *reinterpret_cast<const v2i *>(xp[mt] + kt * x_slab + j * x_step);
-                            xv[j] = v4i{v.x, v.y, 0, 0};
-                        } else {
-                            xv[j] = *reinterpret_cast<const v4i *>(xp[mt] + kt * x_slab + j * x_step);
-                        }
-                    }
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        v4i wd = wv[rt][u];
-                        by_group<GT>(wd);
-                        v4i acc = {0, 0, 0, 0};
-#pragma unroll
-                        for (int j = 0; j < STEPS; ++j) {
-                            if constexpr (GT == 4) {
-                                const v2i b = widen1(wd[j]);
-                                acc = __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, v2i{xv[j].x, xv[j].y}), __builtin_bit_cast(long, b), v4i{0, 0, 0, 0}, 0, 0, 0);
-                            } else {
-                                acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(xv[j], widen2(wd[2 * j], wd[2 * j + 1]), GT == 2 ? v4i{0, 0, 0, 0} : acc, 0, 0, 0);
-                            }
-                            if (GT != 1 || j == 1) {
-                                const float s = sv[rt][u][GT == 1 ? 0 : j];
-#pragma unroll
-                                for (int r = 0; r < 4; ++r) sum[rt][mt][r] = __builtin_fmaf((float)acc[r], s, sum[rt][mt][r]);
-                            }
-                        }
-                    }
-                }
-            }
+        }
     }
 
     // lane l, register r holds token 4 (l / 16) + r, channel l % 16
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) red[wave][(mt * 16 + 4 * q + r) * (16 * RT) + rt * 16 + c] = sum[rt][mt][r];
+        for (int r = 0; r < 4; ++r) red[wave][(4 * q + r) * (16 * RT) + rt * 16 + c] = sum[rt][r];
     __syncthreads();
-    for (int o = tid; o < RT * MT * 256; o += 64 * WAVES) {
-        float v = red[0][o];
+    if (!stores) return;
+    float v = red[0][tid];
 #pragma unroll
-        for (int i = 1; i < WAVES; ++i) v += red[i][o];
-        const int t = m0 + o / (16 * RT), n = n0 + o % (16 * RT);
-        if (t < M && n < N) {
-            v *= token_scale[t] * 0.0625f;
-            if (y_type == FPTQ_F32)
-                static_cast<float *>(y)[(int64_t)t * N + n] = v;
-            else
-                static_cast<uint16_t *>(y)[(int64_t)t * N + n] = bf16_rne(v);
-        }
-    }
+    for (int i = 1; i < WAVES; ++i) v += red[i][tid];
+    v *= ts;
+    if (y_type == FPTQ_F32)
+        static_cast<float *>(y)[(int64_t)t_out * N + n_out] = v;
+    else
+        static_cast<uint16_t *>(y)[(int64_t)t_out * N + n_out] = bf16_rne(v);
 }
 
 // ---- tiles, for more tokens than a few
@@ -159,28 +137,48 @@ __global__ __launch_bounds__(64 * WAVES) void grouped_few_kernel(const uint8_t *
 // by loads that write LDS directly, STAGES deep, one barrier a K tile.  v_mfma_i32_32x32x32_i8 makes a group's integer sums, which go into the fp32 sums at once: with tokens
 // as rows of the result and channels as columns a lane has one channel of a sub-tile, so its scale is one register, and (float)sum and a fused multiply-add are the 32
 // vector instructions that 4 MFMAs (128 cycles) of a 128-value group cost.  Two waves a SIMD, so that one's conversions run under the other's MFMAs.
+// KS sets of WAVES waves share the tile, set g taking K tiles g, g + KS, ... through a ring of its own; with one wave in a set nobody waits for another before the end.
 typedef int v16i __attribute__((ext_vector_type(16)));
 
-template <int WAVES_N_, int WAVES_M_, int TN_, int TM_, int STAGES_, int GT_>
+template <int WAVES_N_, int WAVES_M_, int TN_, int TM_, int STAGES_, int KS_, int GT_>
 struct Tile {
-    static constexpr int WAVES_N = WAVES_N_, WAVES_M = WAVES_M_, TN = TN_, TM = TM_, STAGES = STAGES_, GT = GT_;
-    static constexpr int BN = WAVES_N * TN * 32, BM = WAVES_M * TM * 32, WAVES = WAVES_N * WAVES_M, THREADS = 64 * WAVES;
+    static constexpr int WAVES_N = WAVES_N_, WAVES_M = WAVES_M_, TN = TN_, TM = TM_, STAGES = STAGES_, KS = KS_, GT = GT_;
+    static constexpr int BN = WAVES_N * TN * 32, BM = WAVES_M * TM * 32, WAVES = WAVES_N * WAVES_M, THREADS = 64 * WAVES * KS;
     static constexpr int X_BYTES = BM * KT, W_BYTES = BN * SEG, S_BYTES = BN * GT * 4, STAGE_BYTES = X_BYTES + W_BYTES + S_BYTES;
     static constexpr int X_LOADS = X_BYTES / (WAVES * 1024), W_LOADS = W_BYTES / (WAVES * 1024), S_PIECES = BN * GT / 64, S_LOADS = (S_PIECES + WAVES - 1) / WAVES;
-    static constexpr int LOADS = X_LOADS + W_LOADS + S_LOADS, LDS_BYTES = STAGES * STAGE_BYTES;
+    static constexpr int LOADS = X_LOADS + W_LOADS + S_LOADS, RING_BYTES = STAGES * STAGE_BYTES;
+    static constexpr int SETS = TN * TM * 16 <= 96 && TM > 1 ? 2 : 1;
+    static constexpr int OUT_ROWS = WAVES_M * 32, OUT_BYTES = KS * OUT_ROWS * BN * 4;      // a pass of the epilogue
+    static constexpr int LDS_BYTES = KS * RING_BYTES > OUT_BYTES ? KS * RING_BYTES : OUT_BYTES;
     static_assert(X_BYTES % (WAVES * 1024) == 0 && W_BYTES % (WAVES * 1024) == 0 && BN % 64 == 0, "a K tile is shared out evenly");
     static_assert(S_PIECES % WAVES == 0 || WAVES % S_PIECES == 0, "waves without a piece of their own repeat another's");
     static_assert(LOADS * (STAGES - 1) < 64, "the count of loads in flight has six bits");
+    static_assert(LDS_BYTES <= 160 * 1024 && OUT_ROWS * BN / 4 % THREADS == 0, "");
 };
+
+// where a K tile comes from and goes to
+struct Fill {
+    __amdgpu_buffer_rsrc_t x, w;
+    uint8_t *base;
+    int first, live;      // its first group; whether it is one
+};
+
+template <class F, int... I>
+__device__ inline void in_order(std::integer_sequence<int, I...>, F f)
+{
+    (f(std::integral_constant<int, I>()), ...);
+}
 
 template <class C>
 __global__ __launch_bounds__(C::THREADS, 2) void grouped_tile_kernel(const uint8_t *__restrict__ x, const uint8_t *__restrict__ w, const float *__restrict__ scales, int M, int N,
-                                                                  int ktiles, int tiles_m, int tiles_n, uint32_t tiles_per_group, uint32_t reciprocal_of_it, int groups,
-                                                                  const float *__restrict__ token_scale, void *__restrict__ y, int y_type)
+                                                                     int ktiles, int tiles_m, int tiles_n, uint32_t tiles_per_group, uint32_t reciprocal_of_it, int groups,
+                                                                     const float *__restrict__ token_scale, void *__restrict__ y, int y_type)
 {
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, wave_all = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kg = C::KS > 1 ? wave_all / C::WAVES : 0, wave = C::KS > 1 ? wave_all % C::WAVES : wave_all;
     const int wave_n = wave % C::WAVES_N, wave_m = wave / C::WAVES_N, i32 = lane & 31, h = lane >> 5;
+    uint8_t *const ring = lds + kg * C::RING_BYTES;
 
     // Workgroups go round the 8 XCDs; each gets a contiguous run of tiles, in bands of 8 along n, so that tiles that run together share operands in its L2.
     const int total = tiles_m * tiles_n;
@@ -198,27 +196,30 @@ __global__ __launch_bounds__(C::THREADS, 2) void grouped_tile_kernel(const uint8
     const uint8_t *const x0 = x + (int64_t)m0 * KT, *const w0 = w + (int64_t)n0 * SEG;
     const int x_bytes = min(C::BM, M - m0) * KT, w_bytes = min(C::BN, N - n0) * SEG, s_bytes = min(C::BN, N - n0) * 4;
     const int x_even = wave * C::X_LOADS * 1024 + (lane >> 3) * KT, w_voff = wave * C::W_LOADS * 1024 + (lane >> 2) * SEG + (((lane & 3) ^ ((lane >> 4) & 3)) << 4);
-    auto fill = [&](int kt, int stage) {
-        uint8_t *const base = lds + stage * C::STAGE_BYTES;
-        const bool live = kt < ktiles;
+    // the fills come in order, so that an addition makes the next addresses
+    const uint8_t *x_next = x0 + kg * x_slab, *w_next = w0 + kg * w_slab;
+    int kt_next = kg;
+    auto next_fill = [&](int stage, Fill &f) {
+        f.live = kt_next < ktiles;
+        f.x = __builtin_amdgcn_make_buffer_rsrc((void *)x_next, 0, f.live ? x_bytes : 0, RSRC_FLAGS);
+        f.w = __builtin_amdgcn_make_buffer_rsrc((void *)w_next, 0, f.live ? w_bytes : 0, RSRC_FLAGS);
         uint32_t first, rest;
-        divide((uint32_t)kt, tiles_per_group, reciprocal_of_it, first, rest);
-        const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc((void *)(x0 + kt * x_slab), 0, live ? x_bytes : 0, RSRC_FLAGS);
-        const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc((void *)(w0 + kt * w_slab), 0, live ? w_bytes : 0, RSRC_FLAGS);
-#pragma unroll
-        for (int j = 0; j < C::X_LOADS; ++j) {
-            const int chunk = wave * C::X_LOADS + j, turn = ((chunk & 1) * 4 + (lane >> 4)) & 7;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, LDS_PTR(base + chunk * 1024), 16, x_even + j * 1024 + (((lane & 7) ^ turn) << 4), 0, 0, 0);
-        }
-#pragma unroll
-        for (int j = 0; j < C::W_LOADS; ++j)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, LDS_PTR(base + C::X_BYTES + (wave * C::W_LOADS + j) * 1024), 16, w_voff + j * 1024, 0, 0, 0);
-#pragma unroll
-        for (int j = 0; j < C::S_LOADS; ++j) {
-            const int piece = (wave * C::S_LOADS + j) % C::S_PIECES, g = piece / (C::BN / 64), part = piece % (C::BN / 64);
-            const int group = (int)first * C::GT + g;
-            const __amdgpu_buffer_rsrc_t sr = __builtin_amdgcn_make_buffer_rsrc((void *)(scales + (int64_t)min(group, groups - 1) * N + n0), 0, live ? s_bytes : 0, RSRC_FLAGS);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(sr, LDS_PTR(base + C::X_BYTES + C::W_BYTES + piece * 256), 4, (part * 64 + lane) * 4, 0, 0, 0);
+        divide((uint32_t)kt_next, tiles_per_group, reciprocal_of_it, first, rest);
+        f.base = ring + stage * C::STAGE_BYTES, f.first = (int)first * C::GT;
+        x_next += C::KS * x_slab, w_next += C::KS * w_slab, kt_next += C::KS;
+    };
+    // load j of a fill
+    auto fill = [&](const Fill &f, int j) {
+        if (j < C::W_LOADS) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(f.w, LDS_PTR(f.base + C::X_BYTES + (wave * C::W_LOADS + j) * 1024), 16, w_voff + j * 1024, 0, 0, 0);
+        } else if (j < C::W_LOADS + C::X_LOADS) {
+            const int i = j - C::W_LOADS, chunk = wave * C::X_LOADS + i, turn = ((chunk & 1) * 4 + (lane >> 4)) & 7;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(f.x, LDS_PTR(f.base + chunk * 1024), 16, x_even + i * 1024 + (((lane & 7) ^ turn) << 4), 0, 0, 0);
+        } else {
+            const int i = j - C::W_LOADS - C::X_LOADS, piece = (wave * C::S_LOADS + i) % C::S_PIECES, part = piece % (C::BN / 64);
+            const int group = min(f.first + piece / (C::BN / 64), groups - 1);      // a last tile may hold fewer groups: its weights there are zero
+            const __amdgpu_buffer_rsrc_t sr = __builtin_amdgcn_make_buffer_rsrc((void *)(scales + (int64_t)group * N + n0), 0, f.live ? s_bytes : 0, RSRC_FLAGS);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(sr, LDS_PTR(f.base + C::X_BYTES + C::W_BYTES + piece * 256), 4, (part * 64 + lane) * 4, 0, 0, 0);
         }
     };
 
@@ -230,165 +231,329 @@ __global__ __launch_bounds__(C::THREADS, 2) void grouped_tile_kernel(const uint8
 #pragma unroll
             for (int r = 0; r < 16; ++r) sum[tn][tm][r] = 0.0f;
 
+    // ---- A K tile is UNITS units: the MFMAs of one group of one sub-tile.  While those of a unit run, the sums of the unit before are converted and added
+    // (VALU instructions behind each MFMA, pinned there), the tokens' operands of the next sub-tile are read, into the registers of those that the unit is the last to use or,
+    // where there is room, into others and a unit earlier, and loads of a later K tile are issued.
+    constexpr int MFMAS = 4 / C::GT, UNITS = C::TN * C::TM * C::GT, LAST = UNITS - 1, FIRST = UNITS > 2 ? 1 : 0, PER_UNIT = (C::LOADS + LAST - FIRST - 1) / (LAST - FIRST);
+    static_assert(UNITS % 2 == 0, "units take two sets of accumulators in turn");
+    v16i acc[2] = {};
+    v4i xo[C::SETS][4], wo[C::TN][4], raw[C::TN][2];
+    float sc[C::TN][C::GT], sc_last = 0.0f;
+    const int steps = (ktiles + C::KS - 1) / C::KS;      // the same for all sets: they share the barriers
 #pragma unroll
-    for (int s = 0; s < C::STAGES - 1; ++s) fill(s, s);
+    for (int s = 0; s < C::STAGES - 1; ++s) {
+        Fill f;
+        next_fill(s, f);
+#pragma unroll
+        for (int j = 0; j < C::LOADS; ++j) fill(f, j);
+    }
+    const int x_turn = (i32 >> 1) & 7, w_turn = (i32 >> 2) & 3;
+    const int x_at = (wave_m * C::TM * 32 + i32) * KT, w_at = C::X_BYTES + (wave_n * C::TN * 32 + i32) * SEG, s_at = C::X_BYTES + C::W_BYTES + (wave_n * C::TN * 32 + i32) * 4;
+    // operand m of a K tile covers k = 64 (m / 2) + 32 h + 16 (m % 2) ..., or 32 m + 16 h ... where a group has 32 values
+    auto read_x = [&](const uint8_t *base, int tm, int m) {
+        const int granule = C::GT == 4 ? 2 * m + h : 4 * (m / 2) + 2 * h + m % 2;
+        xo[tm % C::SETS][m] = *reinterpret_cast<const v4i *>(base + x_at + tm * 32 * KT + ((granule ^ x_turn) << 4));
+    };
+    auto read_w = [&](const uint8_t *base) {
+#pragma unroll
+        for (int tn = 0; tn < C::TN; ++tn)
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+                const uint8_t *const row = base + w_at + tn * 32 * SEG;
+                if constexpr (C::GT == 4) {
+                    const v2i p = *reinterpret_cast<const v2i *>(row + (((2 * kk) ^ w_turn) << 4) + 8 * h), q = *reinterpret_cast<const v2i *>(row + (((2 * kk + 1) ^ w_turn) << 4) + 8 * h);
+                    raw[tn][kk] = v4i{p.x, p.y, q.x, q.y};
+                } else {
+                    raw[tn][kk] = *reinterpret_cast<const v4i *>(row + (((2 * kk + h) ^ w_turn) << 4));
+                }
+            }
+    };
+    auto read_scales = [&](const uint8_t *base) {
+#pragma unroll
+        for (int tn = 0; tn < C::TN; ++tn)
+#pragma unroll
+            for (int g = 0; g < C::GT; ++g) sc[tn][g] = *reinterpret_cast<const float *>(base + s_at + (g * C::BN + tn * 32) * 4);
+    };
+    auto widen = [&](int tn) {
+#pragma unroll
+        for (int m = 0; m < 4; ++m) wo[tn][m] = widen2(raw[tn][m / 2][m % 2 * 2], raw[tn][m / 2][m % 2 * 2 + 1]);
+    };
+    auto convert = [&](const v16i &a, float s, float (&f)[16]) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) f[r] = __builtin_fmaf((float)a[r], s, f[r]);
+    };
     int stage = 0;
-    for (int kt = 0; kt < ktiles; ++kt) {
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm(C::LOADS * (C::STAGES - 2)));      // this wave's loads of tile kt are in
-        __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);                                    // and its reads of tile kt - 1
-        __builtin_amdgcn_s_barrier();                                              // everybody's are, and everybody is done with tile kt - 1
+    for (int step = 0; step < steps; ++step) {
+        const uint8_t *const base = ring + stage * C::STAGE_BYTES;
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(C::LOADS * (C::STAGES - 2)));      // this wave's loads of this K tile are in
+        __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);                                    // and its reads of the one before
+        if (C::WAVES > 1) __builtin_amdgcn_s_barrier();                            // everybody's are
         __builtin_amdgcn_sched_barrier(0);
-        fill(kt + C::STAGES - 1, stage == 0 ? C::STAGES - 1 : stage - 1);
-        const uint8_t *const base = lds + stage * C::STAGE_BYTES;
-        const uint8_t *const xb = base + (wave_m * C::TM * 32 + i32) * KT;
-        const uint8_t *const wb = base + C::X_BYTES + (wave_n * C::TN * 32 + i32) * SEG;
-        const float *const sb = reinterpret_cast<const float *>(base + C::X_BYTES + C::W_BYTES) + wave_n * C::TN * 32 + i32;
-        const int x_turn = (i32 >> 1) & 7, w_turn = (i32 >> 2) & 3;
-
-        // operand m of a K tile covers k = 64 (m / 2) + 32 h + 16 (m % 2) ..., or 32 m + 16 h ... where a group has 32 values
-        v4i wo[C::TN][4];
-        float sc[C::TN][C::GT];
+        read_w(base);
 #pragma unroll
-        for (int tn = 0; tn < C::TN; ++tn) {
-            if constexpr (C::GT == 4) {
+        for (int m = 0; m < 4; ++m) read_x(base, 0, m);
+        read_scales(base);
+        widen(0);
+        Fill next;
+        next_fill(stage == 0 ? C::STAGES - 1 : stage - 1, next);
+        in_order(std::make_integer_sequence<int, UNITS>(), [&](auto unit) {
+            constexpr int u = decltype(unit)::value, tm = u / (C::TN * C::GT), tn = u / C::GT % C::TN, g = u % C::GT, p = (u + LAST) % UNITS;
+            constexpr bool reads = tn == (C::SETS == 1 ? C::TN - 1 : 0) && tm + 1 < C::TM, widening = tm == 0 && g == 0 && tn + 1 < C::TN;
+            constexpr int at = (u - FIRST) * PER_UNIT, loads = u < FIRST || at >= C::LOADS ? 0 : C::LOADS - at < PER_UNIT ? C::LOADS - at : PER_UNIT;
+            constexpr int valu = (32 + (widening ? 24 : 0) + MFMAS - 1) / MFMAS;
+            v16i a = {};
 #pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    const v2i p = *reinterpret_cast<const v2i *>(wb + tn * 32 * SEG + ((m ^ w_turn) << 4) + 8 * h);
-                    wo[tn][m] = widen2(p.x, p.y);
-                }
-            } else {
+            for (int m = 0; m < MFMAS; ++m) a = __builtin_amdgcn_mfma_i32_32x32x32_i8(xo[tm % C::SETS][g * MFMAS + m], wo[tn][g * MFMAS + m], a, 0, 0, 0);
+            convert(acc[p % 2], u == 0 ? sc_last : sc[p / C::GT % C::TN][p % C::GT], sum[p / C::GT % C::TN][p / (C::TN * C::GT)]);
+            acc[u % 2] = a;
+            if constexpr (widening) widen(tn + 1);
+            if constexpr (reads) {
 #pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
-                    const v4i p = *reinterpret_cast<const v4i *>(wb + tn * 32 * SEG + (((2 * kk + h) ^ w_turn) << 4));
-                    wo[tn][2 * kk] = widen2(p.x, p.y), wo[tn][2 * kk + 1] = widen2(p.z, p.w);
-                }
+                for (int m = 0; m < MFMAS; ++m) read_x(base, tm + 1, g * MFMAS + m);
             }
 #pragma unroll
-            for (int g = 0; g < C::GT; ++g) sc[tn][g] = sb[g * C::BN + tn * 32];
-        }
+            for (int j = 0; j < loads; ++j) fill(next, at + j);
 #pragma unroll
-        for (int tm = 0; tm < C::TM; ++tm) {
-            v4i xo[4];
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                const int granule = C::GT == 4 ? 2 * m + h : 4 * (m / 2) + 2 * h + m % 2;
-                xo[m] = *reinterpret_cast<const v4i *>(xb + tm * 32 * KT + ((granule ^ x_turn) << 4));
+            for (int m = 0; m < MFMAS; ++m) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                if (reads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                if (loads > 0 && m == 0) __builtin_amdgcn_sched_group_barrier(0x010, loads > 0 ? loads : 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, valu, 0);
             }
-#pragma unroll
-            for (int tn = 0; tn < C::TN; ++tn) {
-#pragma unroll
-                for (int g = 0; g < C::GT; ++g) {
-                    v16i acc = {};
-#pragma unroll
-                    for (int m = 0; m < 4 / C::GT; ++m) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(xo[g * (4 / C::GT) + m], wo[tn][g * (4 / C::GT) + m], acc, 0, 0, 0);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) sum[tn][tm][r] = __builtin_fmaf((float)acc[r], sc[tn][g], sum[tn][tm][r]);
-                }
-            }
-        }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        sc_last = sc[C::TN - 1][C::GT - 1];
         stage = stage + 1 == C::STAGES ? 0 : stage + 1;
     }
-
+    convert(acc[LAST % 2], sc_last, sum[C::TN - 1][C::TM - 1]);
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));      // loads past the last tile, which write LDS
 
-    // ---- register r of lane (i, h) is token 8 (r / 4) + 4 h + r % 4, channel i of its sub-tile.  bf16: neighbouring lanes exchange, so that each has two channels of one token.
+    // ---- epilogue, 32 tokens of each wave at a time: the sums go to LDS as [set][token][channel] and come back four channels of a token to a thread, whose sets it
+    // adds in order.  Register r of lane (i, h) is token 8 (r / 4) + 4 h + r % 4, channel i of its sub-tile.
+    float *const out = reinterpret_cast<float *>(lds);
+    constexpr int PIECES = C::OUT_ROWS * C::BN / 4 / C::THREADS, SET = C::OUT_ROWS * C::BN;
+    const int n = n0 + (tid * 4) % C::BN;
 #pragma unroll
     for (int tm = 0; tm < C::TM; ++tm) {
-        const int t0 = m0 + (wave_m * C::TM + tm) * 32 + 4 * h;
-        float ts[16];
+        __syncthreads();
 #pragma unroll
-        for (int r = 0; r < 16; ++r) ts[r] = token_scale[min(t0 + 8 * (r / 4) + r % 4, M - 1)] * 0.0625f;
+        for (int tn = 0; tn < C::TN; ++tn)
 #pragma unroll
-        for (int tn = 0; tn < C::TN; ++tn) {
-            const int n = n0 + (wave_n * C::TN + tn) * 32 + i32;
+            for (int r = 0; r < 16; ++r)
+                out[kg * SET + (wave_m * 32 + 8 * (r / 4) + 4 * h + r % 4) * C::BN + (wave_n * C::TN + tn) * 32 + i32] = sum[tn][tm][r];
+        __syncthreads();
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            const int at = (p * C::THREADS + tid) * 4, row = at / C::BN, t = m0 + (row / 32 * C::TM + tm) * 32 + row % 32;
+            if (t >= M || n >= N) continue;
+            v4f v = *reinterpret_cast<const v4f *>(out + at);
+#pragma unroll
+            for (int k = 1; k < C::KS; ++k) v += *reinterpret_cast<const v4f *>(out + k * SET + at);
+            const float ts = token_scale[t] * 0.0625f;
+            v *= ts;
             if (y_type == FPTQ_F32) {
-                float *const out = static_cast<float *>(y);
+                float *const to = static_cast<float *>(y) + (int64_t)t * N + n;
+                if (n + 4 <= N) {
+                    __builtin_memcpy(to, &v, 16);
+                } else {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int t = t0 + 8 * (r / 4) + r % 4;
-                    if (t < M && n < N) out[(int64_t)t * N + n] = sum[tn][tm][r] * ts[r];
+                    for (int e = 0; e < 3; ++e)
+                        if (n + e < N) to[e] = v[e];
                 }
             } else {
-                uint16_t *const out = static_cast<uint16_t *>(y);
+                uint16_t *const to = static_cast<uint16_t *>(y) + (int64_t)t * N + n;
+                const uint32_t pair[2] = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+                if (n + 4 <= N) {
+                    __builtin_memcpy(to, pair, 8);
+                } else {
 #pragma unroll
-                for (int r = 0; r < 16; r += 2) {
-                    const float a = sum[tn][tm][r] * ts[r], b = sum[tn][tm][r + 1] * ts[r + 1];
-                    const bool odd = lane & 1;
-                    const float theirs = __uint_as_float(other_lane<1>(__float_as_uint(odd ? a : b)));
-                    const uint32_t pair = odd ? pack_bf16(theirs, b) : pack_bf16(a, theirs);
-                    const int t = t0 + 8 * (r / 4) + r % 4 + (odd ? 1 : 0), c = n & ~1;
-                    if (t < M) {
-                        uint16_t *const to = out + (int64_t)t * N + c;
-                        if (c + 1 < N)
-                            __builtin_memcpy(to, &pair, 4);
-                        else if (c < N)
-                            *to = (uint16_t)pair;
-                    }
+                    for (int e = 0; e < 3; ++e)
+                        if (n + e < N) to[e] = (uint16_t)(pair[e / 2] >> (16 * (e % 2)));
                 }
             }
         }
     }
 }
 
-template <int GT> using Large = Tile<4, 2, 2, 4, 3, GT>;      // 256 x 256
-template <int GT> using Small = Tile<2, 2, 2, 2, 3, GT>;      // 128 x 128, two workgroups a CU
+// ---- which kernel
+//
+// What a tile shape's launch takes, in us, fitted on 2288 launches of random sizes (17 to 6000 tokens, 256 to 60000 channels, K up to 16384, groups of 128 and
+// more, weights not in any cache) on an MI355X: `start`, and for every CU, FIT workgroups at a time, `fixed` and `step` a K tile of a set, which depend on how many run there
+// together.  With groups of 64 the same choice is within 1 % of the best on average, with groups of 32 a step takes about 1.8 times as long.
+struct TileCost {
+    int bn, bm, sets, fit;
+    float start, fixed[3], step[3];
+};
+constexpr TileCost COSTS[] = {
+    {256, 256, 1, 1, 0.0f, {11.78f}, {1.66f}},
+    {256, 192, 1, 1, 0.0f, {9.32f}, {1.36f}},
+    {256, 64, 2, 1, 0.65f, {4.27f}, {1.13f}},
+    {128, 64, 1, 3, 3.17f, {0.81f, 1.82f, 3.26f}, {0.49f, 0.74f, 0.96f}},
+    {128, 64, 2, 1, 0.92f, {2.89f}, {0.64f}},
+    {128, 32, 2, 2, 2.12f, {0.76f, 2.26f}, {0.56f, 0.79f}},
+    {64, 64, 4, 1, 1.15f, {2.81f}, {0.74f}},
+    {64, 32, 8, 1, 0.93f, {2.16f}, {0.77f}},
+};
+template <int GT> using Tile0 = Tile<4, 2, 2, 4, 3, 1, GT>;
+template <int GT> using Tile1 = Tile<4, 2, 2, 3, 3, 1, GT>;
+template <int GT> using Tile2 = Tile<4, 1, 2, 2, 3, 2, GT>;
+template <int GT> using Tile3 = Tile<2, 2, 2, 1, 3, 1, GT>;
+template <int GT> using Tile4 = Tile<4, 1, 1, 2, 3, 2, GT>;
+template <int GT> using Tile5 = Tile<2, 1, 2, 1, 3, 2, GT>;
+template <int GT> using Tile6 = Tile<1, 1, 2, 2, 3, 4, GT>;
+template <int GT> using Tile7 = Tile<1, 1, 2, 1, 2, 8, GT>;
+// groups of 32: the first would spill, the third has no room for its scales in LDS
+constexpr bool tile_serves(int i, int gt) { return gt < 4 || (i != 0 && i != 2); }
 
-template <class... Cs>
+static float tile_estimate(const TileCost &c, int64_t M, int64_t N, int64_t kt, int64_t cus, int gt)
+{
+    const int64_t each = (((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn) + cus - 1) / cus, full = each / c.fit, rest = each % c.fit;      // workgroups of a CU
+    const float steps = (float)((kt + c.sets - 1) / c.sets) * (gt == 4 ? 1.8f : 1.0f);
+    return c.start + (float)full * (c.fixed[c.fit - 1] + steps * c.step[c.fit - 1]) + (rest ? c.fixed[rest - 1] + steps * c.step[rest - 1] : 0.0f);
+}
+
+// The few-token kernels the same way: a start, and for every K tile of a wave a latency or what the workgroups of a CU take together.
+struct FewCost {
+    int waves, channels;
+    float start, latency, each;
+};
+constexpr FewCost FEW_COSTS[] = {{16, 16, 2.07f, 0.70f, 0.87f}, {16, 32, 1.96f, 0.98f, 1.27f}, {8, 32, 2.15f, 0.68f, 0.71f}, {8, 16, 0.0f, 0.0f, 0.0f}};
+
+static float few_estimate(const FewCost &c, int64_t M, int64_t N, int64_t kt, int64_t cus, int gt)
+{
+    const float steps = (float)((kt + c.waves - 1) / c.waves) * (gt == 4 ? 1.5f : 1.0f), n = (float)((N + c.channels - 1) / c.channels * ((M + 15) / 16)) / (float)cus;
+    return c.start + steps * (c.each * n > c.latency ? c.each * n : c.latency);
+}
+
+// The kernel of a call: 0 .. 7 a tile, 8 + i the few-token kernel FEW_COSTS[i].  Up to 16 tokens, on 10188 matrices of up to 130000 channels with groups of 128 and 64, by two lines:
+// short K wants eight waves; as many workgroups as CUs or a few times as many want sixteen waves, with 32 channels from 16 * CUs channels on; more workgroups want eight
+// again while K is not long.  us, 16 waves of 16 channels / 16 of 32 / 8 of 16 / 8 of 32: 4096 x 14336 7.8 / 8.9 / 10.6 / 14, 6144 x 4096 5.1 / 4.6 / 4.9 / 5.2, 28672 x 4096 - / 13.2 / 13.5 / 12.3.
+// On each of a grid of sizes the choice is within 5 % of the best of the four on average.
+static int grouped_choice(int64_t M, int64_t N, int64_t K, int gt)
+{
+    const int64_t kt = k_tiles(K), cus = device_cus_or_default();
+    if (M <= 16) {
+        if (kt < 9) return N <= 48 * cus ? 11 : 10;
+        return N <= 16 * cus ? 8 : N > 64 * cus && kt < 33 ? 10 : 9;
+    }
+    // no kernel takes less than its bytes do at 5.4 TB/s; among those that come to it the larger tile reads less (32 x 28672 x 4096, fourth from last 14.4 us, last 17.0)
+    const float bytes = (float)N * (float)kt * (float)(SEG + 4 * gt) + (float)M * (float)kt * (float)KT + 2.0f * (float)M * (float)N, memory = bytes / 5.4e6f;
+    int best = -1;
+    float least = 0.0f;
+    auto offer = [&](int i, float us) {
+        us = us > memory ? us : memory;
+        if (best < 0 || us < least) best = i, least = us;
+    };
+    for (int i = 0; i < 8; ++i)
+        if (tile_serves(i, gt)) offer(i, tile_estimate(COSTS[i], M, N, kt, cus, gt));
+    if (M <= 64)
+        for (int i = 0; i < 3; ++i) offer(8 + i, few_estimate(FEW_COSTS[i], M, N, kt, cus, gt));
+    return best;
+}
+
+template <class C>
+static hipError_t set_tile_attribute()
+{
+    return hipFuncSetAttribute((const void *)grouped_tile_kernel<C>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES);
+}
+template <int GT>
 static hipError_t set_tile_attributes()
 {
     hipError_t e = hipSuccess;
-    ((e = e == hipSuccess ? hipFuncSetAttribute((const void *)grouped_tile_kernel<Cs>, hipFuncAttributeMaxDynamicSharedMemorySize, Cs::LDS_BYTES) : e), ...);
-    return e;
+    if constexpr (tile_serves(0, GT)) e = set_tile_attribute<Tile0<GT>>();
+    if (e == hipSuccess) e = set_tile_attribute<Tile1<GT>>();
+    if constexpr (tile_serves(2, GT)) e = e == hipSuccess ? set_tile_attribute<Tile2<GT>>() : e;
+    if (e == hipSuccess) e = set_tile_attribute<Tile3<GT>>();
+    if (e == hipSuccess) e = set_tile_attribute<Tile4<GT>>();
+    if (e == hipSuccess) e = set_tile_attribute<Tile5<GT>>();
+    if (e == hipSuccess) e = set_tile_attribute<Tile6<GT>>();
+    return e == hipSuccess ? set_tile_attribute<Tile7<GT>>() : e;
 }
-hipError_t grouped_device_init() { return set_tile_attributes<Large<1>, Large<2>, Large<4>, Small<1>, Small<2>, Small<4>>(); }
+hipError_t grouped_device_init()
+{
+    hipError_t e = set_tile_attributes<1>();
+    if (e == hipSuccess) e = set_tile_attributes<2>();
+    return e == hipSuccess ? set_tile_attributes<4>() : e;
+}
+
+struct GroupedCall {
+    const uint8_t *x;
+    const float *token_scale;
+    const uint8_t *w;
+    int M, N, ktiles, groups;
+    uint32_t per;      // K tiles of a group
+    const float *scales;
+    void *y;
+    int y_type;
+    hipStream_t stream;
+};
 
 template <class C>
-static hipError_t launch_tile(const uint8_t *x, const float *token_scale, const uint8_t *w, int64_t M, int64_t N, int64_t K, int64_t groups, int64_t per,
-                              const float *scales, void *y, int y_type, hipStream_t s)
+static hipError_t launch_tile(const GroupedCall &c)
 {
-    const int64_t tiles_m = (M + C::BM - 1) / C::BM, tiles_n = (N + C::BN - 1) / C::BN;
+    const int64_t tiles_m = (c.M + C::BM - 1) / C::BM, tiles_n = (c.N + C::BN - 1) / C::BN;
     if (tiles_m * tiles_n > (int64_t)0xffffffff / C::THREADS) return hipErrorInvalidConfiguration;
     const DeviceInfo *info;
     const hipError_t e = device_info(&info);      // the tiles' LDS is an attribute of the kernels, set once per device
     if (e != hipSuccess) return e;
-    grouped_tile_kernel<C><<<dim3((unsigned)(tiles_m * tiles_n)), dim3(C::THREADS), C::LDS_BYTES, s>>>(x, w, scales, (int)M, (int)N, (int)k_tiles(K), (int)tiles_m,
-                                                                                                       (int)tiles_n, (uint32_t)per, reciprocal((uint32_t)per),
-                                                                                                       (int)groups, token_scale, y, y_type);
+    grouped_tile_kernel<C><<<dim3((unsigned)(tiles_m * tiles_n)), dim3(C::THREADS), C::LDS_BYTES, c.stream>>>(
+        c.x, c.w, c.scales, c.M, c.N, c.ktiles, (int)tiles_m, (int)tiles_n, c.per, reciprocal(c.per), c.groups, c.token_scale, c.y, c.y_type);
     return hipGetLastError();
+}
+
+template <int WAVES, int RT, int GT>
+static hipError_t launch_few(const GroupedCall &c)
+{
+    grouped_few_kernel<WAVES, RT, GT><<<dim3((unsigned)((c.N + 16 * RT - 1) / (16 * RT)), (unsigned)((c.M + 15) / 16)), dim3(64 * WAVES), 0, c.stream>>>(
+        c.x, c.w, c.scales, c.M, c.N, c.ktiles, c.groups, c.per, reciprocal(c.per), c.token_scale, c.y, c.y_type);
+    return hipGetLastError();
+}
+
+template <int GT>
+static hipError_t launch_choice(int choice, const GroupedCall &c)
+{
+    switch (choice) {
+    case 0:
+        if constexpr (tile_serves(0, GT)) return launch_tile<Tile0<GT>>(c);
+        break;
+    case 1: return launch_tile<Tile1<GT>>(c);
+    case 2:
+        if constexpr (tile_serves(2, GT)) return launch_tile<Tile2<GT>>(c);
+        break;
+    case 3: return launch_tile<Tile3<GT>>(c);
+    case 4: return launch_tile<Tile4<GT>>(c);
+    case 5: return launch_tile<Tile5<GT>>(c);
+    case 6: return launch_tile<Tile6<GT>>(c);
+    case 7: return launch_tile<Tile7<GT>>(c);
+    case 8: return launch_few<16, 1, GT>(c);
+    case 9: return launch_few<16, 2, GT>(c);
+    case 10: return launch_few<8, 2, GT>(c);
+    case 11: return launch_few<8, 1, GT>(c);
+    }
+    return hipErrorInvalidValue;
+}
+
+// 0: chosen per problem; 1 + i forces choice i (testing and tuning)
+static std::atomic<int> g_forced_grouped{0};
+bool set_grouped_kernel(int kernel)
+{
+    if (kernel < 0 || kernel > 12) return false;
+    g_forced_grouped.store(kernel, std::memory_order_relaxed);
+    return true;
+}
+int grouped_kernel(int64_t M, int64_t N, int64_t K, int64_t group)
+{
+    const int forced = g_forced_grouped.load(std::memory_order_relaxed);
+    return forced ? forced - 1 : grouped_choice(M, N, K, group == 32 ? 4 : group == 64 ? 2 : 1);
 }
 
 hipError_t launch_grouped_linear(const uint8_t *x, const float *token_scale, const uint8_t *w, int64_t M, int64_t N, int64_t K, int64_t group, const float *scales,
                                  void *y, int y_type, hipStream_t s)
 {
-    const int64_t kt = k_tiles(K), groups = (K + group - 1) / group, per = group > KT ? min(group / KT, kt) : 1;
-    if (M > 64) {
-        const bool large = ((M + 255) / 256) * ((N + 255) / 256) >= 200;
-#define FPTQ_TILE(GT)                                                                                                             \
-    do {                                                                                                                          \
-        if (large) return launch_tile<Large<GT>>(x, token_scale, w, M, N, K, groups, per, scales, y, y_type, s);                  \
-        return launch_tile<Small<GT>>(x, token_scale, w, M, N, K, groups, per, scales, y, y_type, s);                             \
-    } while (0)
-        if (group == 32) FPTQ_TILE(4);
-        if (group == 64) FPTQ_TILE(2);
-        FPTQ_TILE(1);
-#undef FPTQ_TILE
-    }
-#define FPTQ_FEW(MT, GT)                                                                                                                   \
-    do {                                                                                                                                   \
-        grouped_few_kernel<8, 1, MT, 1, GT><<<dim3((unsigned)((N + 15) / 16), (unsigned)((M + 16 * MT - 1) / (16 * MT))), dim3(512), 0, s>>>(   \
-            x, w, scales, (int)M, (int)N, (int)kt, (int)groups, (uint32_t)per, reciprocal((uint32_t)per), token_scale, y, y_type);         \
-        return hipGetLastError();                                                                                                          \
-    } while (0)
-#define FPTQ_FEW_GT(GT)              \
-    do {                             \
-        if (M <= 16) FPTQ_FEW(1, GT); \
-        FPTQ_FEW(4, GT);             \
-    } while (0)
-    if (group == 32) FPTQ_FEW_GT(4);
-    if (group == 64) FPTQ_FEW_GT(2);
-    FPTQ_FEW_GT(1);
-#undef FPTQ_FEW_GT
-#undef FPTQ_FEW
+    const int64_t kt = k_tiles(K), per = group > KT ? (group / KT < kt ? group / KT : kt) : 1;
+    const GroupedCall c = {x, token_scale, w, (int)M, (int)N, (int)kt, (int)((K + group - 1) / group), (uint32_t)per, scales, y, y_type, s};
+    const int choice = grouped_kernel(M, N, K, group);
+    return group == 32 ? launch_choice<4>(choice, c) : group == 64 ? launch_choice<2>(choice, c) : launch_choice<1>(choice, c);
 }
 
 }  // namespace fptq

@@ -63,6 +63,28 @@ def test_products_of_many_tiles(M, N, K, group):
     check(run(*case, group, torch.bfloat16), y, mass, K, group)
 
 
+@pytest.fixture
+def forced():
+    yield fptq.fptq_set_grouped_kernel
+    fptq.fptq_set_grouped_kernel(0)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128, 256])
+@pytest.mark.parametrize("kernel", range(1, 13))
+def test_every_kernel(kernel, group, forced):
+    """Each kernel on sizes that cut its tiles, sets of K tiles and groups; a single K tile, fewer than it has sets, and many."""
+    for M, N, K in ((1, 1, 1), (70, 90, 100), (33, 257, 640), (300, 520, 1100), (257, 129, 2600), (5, 64, 129)):
+        case = draw(M, N, K, group, kernel)
+        y, mass = grouped.linear(*case[:3], group, case[3])
+        forced(kernel)
+        if group == 32 and kernel in (1, 3):
+            with pytest.raises(fptq.FptqError):
+                run(*case, group)
+            continue
+        check(run(*case, group), y, mass, K, group)
+        check(run(*case, group, torch.bfloat16), y, mass, K, group)
+
+
 @pytest.mark.parametrize("M", [1, 40, 300])
 def test_one_scale_a_channel(M):
     N, K = 96, 700

@@ -43,7 +43,7 @@ def test_gated(code, changed):
 
 @pytest.mark.parametrize("code,changed", [
     (NULL, dict(x=None)), (NULL, dict(s=None)), (NULL, dict(w=None)), (NULL, dict(ws=None)), (NULL, dict(y=None)),
-    (SHAPE, dict(M=0)), (SHAPE, dict(N=0)), (SHAPE, dict(K=0)), (SHAPE, dict(M=1 << 25)), (SHAPE, dict(N=(1 << 24) + 1)), (SHAPE, dict(K=1 << 25)),
+    (SHAPE, dict(M=0)), (SHAPE, dict(N=0)), (SHAPE, dict(K=0)), (SHAPE, dict(M=1 << 25)), (SHAPE, dict(N=(1 << 24) + 1)), (SHAPE, dict(K=1 << 25)), (SHAPE, dict(M=1 << 24, N=1 << 14)),
     (SHAPE, dict(group=0)), (SHAPE, dict(group=-128)), (SHAPE, dict(group=16)), (SHAPE, dict(group=96)), (SHAPE, dict(group=130)), (SHAPE, dict(group=192)),
     (MODE, dict(type=2)), (MODE, dict(type=-1)), (ALIGN, dict(x=EIGHT)), (ALIGN, dict(w=EIGHT)), (ALIGN, dict(y=EIGHT)), (ALIGN, dict(s=TWO)), (ALIGN, dict(ws=TWO))])
 def test_linear(code, changed):
@@ -56,3 +56,18 @@ def test_sizes_and_unpack():
     assert L.fptq_packed8_bytes(0, 1) == SHAPE and L.fptq_packed8_bytes(1, -1) == SHAPE
     assert L.fptq_unpack8(None, 1, 1, P, None) == NULL and L.fptq_unpack8(P, 1, 1, None, None) == NULL
     assert L.fptq_unpack8(P, 0, 1, P, None) == SHAPE and L.fptq_unpack8(EIGHT, 1, 1, P, None) == ALIGN
+
+
+def test_kernel_choice_is_host_arithmetic():
+    """On 256 CUs: a few-token kernel up to 16 tokens by two lines, then the least of the fitted times."""
+    L = fptq.lib()
+    for bad in (-1, 13):
+        assert L.fptq_set_grouped_kernel(bad) == VALUE
+    of = L.fptq_grouped_kernel
+    assert of(0, 1, 1, 32) == SHAPE and of(1, 1, 1, 0) == SHAPE
+    assert of(1, 4096, 4096, 128) == 9 and of(1, 6144, 4096, 128) == 10 and of(8, 128256, 4096, 64) == 11 and of(16, 28672, 14336, 128) == 10 and of(3, 4096, 512, 128) == 12
+    assert of(4096, 28672, 4096, 128) == 1 and of(333, 32003, 2504, 64) == 2 and of(1000, 4096, 14336, 128) == 3 and of(32, 28672, 4096, 128) == 6
+    for M in (17, 64, 65, 500, 3000):
+        for N in (64, 1000, 5000, 40000):
+            for K in (128, 1000, 8000):
+                assert of(M, N, K, 32) not in (1, 3) and 1 <= of(M, N, K, 128) <= (11 if M <= 64 else 8)
