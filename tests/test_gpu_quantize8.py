@@ -11,7 +11,8 @@ from paper_2506_04985_amd import binding as fptq
 
 pytestmark = pytest.mark.gpu
 
-SHAPES = [(1, 1), (1, 7), (2, 8), (3, 9), (5, 127), (4, 128), (3, 129), (1, 2048), (2, 2056), (1, 4096), (7, 4100), (3, 4099), (1030, 63), (1030, 512), (1100, 515),
+SHAPES = [(2050, 700), (2049, 1001), (2051, 1800), (2052, 1801), (1500, 3000), (1501, 3001), (3100, 505), (600, 6001), (513, 6000), (5, 6000), (520, 8000), (300, 13000), (3, 12000), (3, 12001), (2, 20000), (2, 24001),
+          (1, 1), (1, 7), (2, 8), (3, 9), (5, 127), (4, 128), (3, 129), (1, 2048), (2, 2056), (1, 4096), (7, 4100), (3, 4099), (1030, 63), (1030, 512), (1100, 515),
           (1100, 1024), (1027, 1500), (1029, 2048), (2, 8192), (3, 8189), (2, 8200), (1, 16384), (2, 16390), (3, 16383), (2, 28672), (2, 32768), (1, 32761), (1, 32769), (2, 40960)]
 
 
@@ -79,17 +80,24 @@ def test_gated(M, K):
     assert np.array_equal(scale.cpu().numpy(), want_scale)
 
 
-def test_silu_of_every_bf16_value():
-    """With up = 1 and one value a row (and a second one, 0) the scale is |silu(g)| / 127: every finite bf16, compared bit by bit through two roundings that cannot differ."""
-    bits = torch.arange(65536, dtype=torch.int32, device="cuda").to(torch.int16)
-    gate = torch.zeros((65536, 2), dtype=torch.bfloat16, device="cuda")
-    gate[:, 0] = bits.view(torch.bfloat16)
-    up = torch.ones_like(gate)
-    codes, scale = fptq.fptq_gated_quantize8(gate, up)
-    want, want_scale = grouped.quantize_rows(grouped.gated(host(gate), host(up)))
-    assert np.array_equal(scale.cpu().numpy(), want_scale, equal_nan=True)
-    assert np.array_equal(codes.cpu().numpy(), grouped.lay_out(want))
-    assert int(torch.isnan(scale).sum()) == 2 + 2 * 127                 # the infinities and the NaN
+@pytest.mark.parametrize("K", [2, 600, 5000])
+def test_silu_of_every_bf16_value(K):
+    """With up = 1 and one value a row the scale is |silu(g)| / 127: every bf16, through two roundings that cannot differ, and the sign by the code.  In short rows, in rows of the table's
+    kernels, and in rows where it is taken whatever their number."""
+    step = 65536 if K < 5000 else 8192
+    for first in range(0, 65536, step):
+        bits = torch.arange(first, first + step, dtype=torch.int32, device="cuda").to(torch.int16)
+        gate = torch.zeros((step, K), dtype=torch.bfloat16, device="cuda")
+        gate[:, K // 2] = bits.view(torch.bfloat16)
+        up = torch.ones_like(gate)
+        codes, scale = fptq.fptq_gated_quantize8(gate, up)
+        g = host(gate[:, K // 2:K // 2 + 1])
+        want, want_scale = grouped.quantize_rows(grouped.gated(g, np.ones_like(g)))
+        assert np.array_equal(scale.cpu().numpy(), want_scale, equal_nan=True)
+        got = fptq.fptq_unpack8(codes, step, K)
+        assert np.array_equal(got[:, K // 2].cpu().numpy(), want[:, 0])
+        got[:, K // 2] = 0
+        assert not bool(got.any())
 
 
 @pytest.mark.parametrize("M,K", [(9, 40), (1025, 40), (5, 4096), (3, 5000), (2, 20000), (2, 33000)])
@@ -162,13 +170,13 @@ def test_any_alignment_and_any_distance_between_rows(K, shift):
 
 def test_more_rows_than_one_launch_takes():
     """A launch has 2^20 workgroups at most; they go on from row to row."""
-    for M, K in ((4 * (1 << 20) + 5, 8), ((1 << 20) + 3, 72)):
+    for M, K in ((4 * (1 << 20) + 5, 8), ((1 << 20) + 3, 1026)):
         g = torch.Generator(device="cuda").manual_seed(K)
         x = torch.randn((M, K), device="cuda", generator=g).to(torch.bfloat16)
         codes, scale, _ = fptq.fptq_norm_quantize8(x, scale_mode=fptq.SCALE_NONE)
         at = torch.tensor([0, 1, (1 << 20) - 1, 1 << 20, M - 2, M - 1])
         want, want_scale = grouped.quantize_rows(host(x[at.cuda()]))
-        assert np.array_equal(codes.view(1, M, 16, 8)[0][at.cuda()].cpu().numpy().reshape(-1), grouped.lay_out(want))
+        assert np.array_equal(codes.view(-1, M, 128)[:, at.cuda()].cpu().numpy().reshape(-1), grouped.lay_out(want))
         assert np.array_equal(scale[at.cuda()].cpu().numpy(), want_scale)
         del x, codes
         torch.cuda.empty_cache()
