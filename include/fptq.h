@@ -346,17 +346,22 @@ int fptq_gated_quantize8(const void *gate, const void *up, int64_t M, int64_t K,
 
 /*
  * y[t, n] = token_scale[t] * sum_g w_scales[g, n] * (sum over the group's k of code[t, k] * w[n, k]), from one token to long prompts.
- * The inner sums are exact integers; those of the groups are added in fp32, in an order that the shape alone decides.
+ * The inner sums are exact integers; those of the groups are added in fp32, in an order that the shape and the scratch alone decide.
  *   xq8          device, codes from one of the quantizers above
  *   w_packed     device, packed weights [N x K] from fptq_pack_weights
  *   group        values of K to a scale: 32, 64 or a multiple of 128 (of K or more: one scale a channel); the last group may be shorter
  *   w_scales     device, fp32 [ceil(K / group) x N], finite
  *   y            device, 16-byte aligned, [M x N] row-major of y_type: FPTQ_BF16 or FPTQ_F32
+ *   scratch      device, 256-byte aligned, at least fptq_w4a8_linear_scratch_bytes(...) bytes (64 MB at most, 0 for most shapes), or NULL.  With it a long K against few
+ *                outputs is shared out to more workgroups, in two launches.  Too small: as NULL.  Its contents need no initialisation and mean nothing afterwards.
+ *                Calls that share it must not overlap in time.
+ * M and N up to 2^24, M * N up to 2^37.
  */
 #define FPTQ_BF16 0
 #define FPTQ_F32 1
+int64_t fptq_w4a8_linear_scratch_bytes(int64_t M, int64_t N, int64_t K, int64_t group);
 int fptq_w4a8_linear(const void *xq8, const float *token_scale, const void *w_packed, int64_t M, int64_t N, int64_t K, int64_t group,
-                     const float *w_scales, void *y, int y_type, void *stream);
+                     const float *w_scales, void *y, int y_type, void *scratch, int64_t scratch_bytes, void *stream);
 
 /* Codes of 8 bits in the library's layout -> int8 [rows x K] row-major (for parity checks and debugging). */
 int fptq_unpack8(const void *packed8, int64_t rows, int64_t K, int8_t *out_int8, void *stream);

@@ -23,7 +23,8 @@ EXPORTS = ["fptq_version", "fptq_last_error", "fptq_init", "fptq_packed_bytes", 
            "fptq_w4a4_linear", "fptq_w4a4_linear_ref", "fptq_unpack", "fptq_linear_workspace_bytes", "fptq_w4a4_linear_ws",
            "fptq_w4a4_linear_noalloc", "fptq_linear_scratch_bytes", "fptq_w4a4_linear_scratch",
            "fptq_cache_append", "fptq_cached_attention_scratch_bytes", "fptq_cached_attention", "fptq_prompt_attention",
-           "fptq_packed8_bytes", "fptq_norm_quantize8", "fptq_gated_quantize8", "fptq_w4a8_linear", "fptq_unpack8"]
+           "fptq_packed8_bytes", "fptq_norm_quantize8", "fptq_gated_quantize8", "fptq_w4a8_linear_scratch_bytes", "fptq_w4a8_linear",
+           "fptq_unpack8"]
 TESTING_EXPORTS = ["fptq_set_gemm_tile", "fptq_set_gemm_map", "fptq_set_decode_shape", "fptq_set_linear_prefill",
                    "fptq_linear_launch_plan", "fptq_set_grouped_kernel", "fptq_grouped_kernel"]
 
@@ -114,10 +115,12 @@ def lib():
         L.fptq_norm_quantize8.argtypes = [p, p, p, i64, i64, i32, f32, p, i64, p, p, p]
         L.fptq_gated_quantize8.restype = i32
         L.fptq_gated_quantize8.argtypes = [p, p, i64, i64, i64, i64, p, i64, p, p]
+        L.fptq_w4a8_linear_scratch_bytes.restype = i64
+        L.fptq_w4a8_linear_scratch_bytes.argtypes = [i64, i64, i64, i64]
         L.fptq_w4a8_linear.restype = i32
-        L.fptq_w4a8_linear.argtypes = [p, p, p, i64, i64, i64, i64, p, p, i32, p]
+        L.fptq_w4a8_linear.argtypes = [p, p, p, i64, i64, i64, i64, p, p, i32, p, i64, p]
         L.fptq_set_grouped_kernel.restype = i32
-        L.fptq_set_grouped_kernel.argtypes = [i32]
+        L.fptq_set_grouped_kernel.argtypes = [i32, i32]
         L.fptq_grouped_kernel.restype = i32
         L.fptq_grouped_kernel.argtypes = [i64, i64, i64, i64]
         L.fptq_unpack8.restype = i32
@@ -606,11 +609,20 @@ def fptq_gated_quantize8(gate, up, out=None, token_scale_out=None):
     return out, token_scale_out
 
 
-def fptq_w4a8_linear(xq8, token_scale, wq, M, N, K, group, w_scales, out=None, out_dtype=torch.bfloat16):
-    """Codes of 8 bits (from one of the quantizers above) x packed 4-bit weights with fp32 [ceil(K / group), N] scales: [M, N] in bf16 or fp32."""
+def fptq_w4a8_linear_scratch_bytes(M, N, K, group):
+    """Bytes of scratch fptq_w4a8_linear would use for this shape (0: it would not use any)."""
+    n = lib().fptq_w4a8_linear_scratch_bytes(M, N, K, group)
+    if n < 0:
+        _check(int(n))
+    return int(n)
+
+
+def fptq_w4a8_linear(xq8, token_scale, wq, M, N, K, group, w_scales, out=None, out_dtype=torch.bfloat16, scratch=None):
+    """Codes of 8 bits (from one of the quantizers above) x packed 4-bit weights with fp32 [ceil(K / group), N] scales: [M, N] in bf16 or fp32.  Scratch comes from torch's
+    allocator unless given: a capture not made through torch, which would have no pool of its own, has to give it."""
     if out_dtype is not torch.bfloat16 and out_dtype is not torch.float32:
         raise TypeError(f"out_dtype: bf16 or fp32, not {out_dtype}")
-    done = None if _native is None else _native.w4a8_linear(xq8, token_scale, wq, M, N, K, group, w_scales, out, out_dtype is torch.float32)
+    done = None if _native is None else _native.w4a8_linear(xq8, token_scale, wq, M, N, K, group, w_scales, out, out_dtype is torch.float32, scratch)
     if done is not None:
         return done
     _dev(xq8, torch.int8, "xq8")
@@ -623,11 +635,19 @@ def fptq_w4a8_linear(xq8, token_scale, wq, M, N, K, group, w_scales, out=None, o
         raise FptqError(-3, "codes, token_scale or packed weights smaller than the shape needs")
     if w_scales.numel() < -(-K // group) * N:
         raise FptqError(-3, f"w_scales: {w_scales.numel()} values, need {-(-K // group)} x {N}")
+    if scratch is None:
+        n = fptq_w4a8_linear_scratch_bytes(M, N, K, group)
+        # as in _scratch: only the order of its own stream guards it once the call has returned
+        if n > 0 and xq8.device.index == torch.cuda.current_device():
+            scratch = torch.empty(n, dtype=torch.uint8, device=xq8.device)
+    else:
+        _dev(scratch, torch.uint8, "scratch")
     if out is None:
         out = torch.empty((M, N), dtype=out_dtype, device=xq8.device)
     elif _dev(out, out_dtype, "out").numel() < M * N:
         raise FptqError(-3, f"out: {out.numel()} values, need {M} x {N}")
-    _check(lib().fptq_w4a8_linear(_ptr(xq8), _ptr(token_scale), _ptr(wq), M, N, K, group, _ptr(w_scales), _ptr(out), int(out_dtype == torch.float32), _stream()))
+    _check(lib().fptq_w4a8_linear(_ptr(xq8), _ptr(token_scale), _ptr(wq), M, N, K, group, _ptr(w_scales), _ptr(out), int(out_dtype is torch.float32), _ptr(scratch),
+                                  0 if scratch is None else scratch.numel(), _stream()))
     return out
 
 
@@ -641,8 +661,8 @@ def fptq_unpack8(packed8, rows, K):
     return out
 
 
-def fptq_set_grouped_kernel(kernel):
-    _check(lib().fptq_set_grouped_kernel(int(kernel)))
+def fptq_set_grouped_kernel(kernel, splits=1):
+    _check(lib().fptq_set_grouped_kernel(int(kernel), int(splits)))
 
 
 def fptq_set_gemm_map(mode):

@@ -745,14 +745,9 @@ int fptq_gated_quantize8(const void *gate, const void *up, int64_t M, int64_t K,
                                                token_scale, (hipStream_t)stream));
 }
 
-int fptq_w4a8_linear(const void *xq8, const float *token_scale, const void *w_packed, int64_t M, int64_t N, int64_t K, int64_t group,
-                     const float *w_scales, void *y, int y_type, void *stream)
+// the sizes of a linear call with 8-bit activations
+static int check_grouped(const char *fn, int64_t M, int64_t N, int64_t K, int64_t group)
 {
-    const char *fn = "fptq_w4a8_linear";
-    if (!xq8 || !token_scale || !w_packed || !w_scales || !y) {
-        set_error("%s: NULL pointer", fn);
-        return FPTQ_ERR_NULL;
-    }
     int rc;
     if ((rc = check_dims(fn, M, K, "M", "K")) || (rc = check_dims(fn, N, K, "N", "K")) || (rc = check_dims(fn, M, N, "M", "N"))) return rc;
     if (group != 32 && group != 64 && (group < 128 || group % 128)) {
@@ -768,27 +763,39 @@ int fptq_w4a8_linear(const void *xq8, const float *token_scale, const void *w_pa
         set_error("%s: M=%lld and N=%lld make more than %lld outputs", fn, (long long)M, (long long)N, (long long)GROUPED_OUTPUTS);
         return FPTQ_ERR_SHAPE;
     }
+    return FPTQ_OK;
+}
+
+int64_t fptq_w4a8_linear_scratch_bytes(int64_t M, int64_t N, int64_t K, int64_t group)
+{
+    const int rc = check_grouped("fptq_w4a8_linear_scratch_bytes", M, N, K, group);
+    return rc ? rc : grouped_scratch_bytes(M, N, K, group);
+}
+
+int fptq_w4a8_linear(const void *xq8, const float *token_scale, const void *w_packed, int64_t M, int64_t N, int64_t K, int64_t group,
+                     const float *w_scales, void *y, int y_type, void *scratch, int64_t scratch_bytes, void *stream)
+{
+    const char *fn = "fptq_w4a8_linear";
+    if (!xq8 || !token_scale || !w_packed || !w_scales || !y) {
+        set_error("%s: NULL pointer", fn);
+        return FPTQ_ERR_NULL;
+    }
+    int rc;
+    if ((rc = check_grouped(fn, M, N, K, group))) return rc;
     if (y_type != FPTQ_BF16 && y_type != FPTQ_F32) {
         set_error("%s: y_type must be FPTQ_BF16 or FPTQ_F32 (got %d)", fn, y_type);
         return FPTQ_ERR_MODE;
     }
-    if ((rc = check_align(fn, xq8, 16, "xq8")) || (rc = check_align(fn, w_packed, 16, "w_packed")) || (rc = check_align(fn, y, 16, "y")) ||
-        (rc = check_align(fn, token_scale, 4, "token_scale")) || (rc = check_align(fn, w_scales, 4, "w_scales")))
-        return rc;
-    return launched(fn, launch_grouped_linear((const uint8_t *)xq8, token_scale, (const uint8_t *)w_packed, M, N, K, group, w_scales, y, y_type,
-                                              (hipStream_t)stream));
-}
-
-int fptq_set_grouped_kernel(int kernel)
-{
-    if (!set_grouped_kernel(kernel)) {
-        set_error("fptq_set_grouped_kernel: kernel must be 0..12");
-        return FPTQ_ERR_VALUE;
+    if (scratch_bytes < 0) {
+        set_error("%s: negative scratch_bytes", fn);
+        return FPTQ_ERR_SIZE;
     }
-    return FPTQ_OK;
+    if ((rc = check_align(fn, xq8, 16, "xq8")) || (rc = check_align(fn, w_packed, 16, "w_packed")) || (rc = check_align(fn, y, 16, "y")) ||
+        (rc = check_align(fn, token_scale, 4, "token_scale")) || (rc = check_align(fn, w_scales, 4, "w_scales")) || (rc = check_align(fn, scratch, 256, "scratch")))
+        return rc;
+    return launched(fn, launch_grouped_linear((const uint8_t *)xq8, token_scale, (const uint8_t *)w_packed, M, N, K, group, w_scales, y, y_type, scratch,
+                                              scratch_bytes, (hipStream_t)stream));
 }
-
-int fptq_grouped_kernel(int64_t M, int64_t N, int64_t K, int64_t group) { return M < 1 || N < 1 || K < 1 || group < 1 ? FPTQ_ERR_SHAPE : 1 + grouped_kernel(M, N, K, group); }
 
 int fptq_unpack8(const void *packed8, int64_t rows, int64_t K, int8_t *out_int8, void *stream)
 {
@@ -801,5 +808,16 @@ int fptq_unpack8(const void *packed8, int64_t rows, int64_t K, int8_t *out_int8,
     if ((rc = check_dims(fn, rows, K, "rows", "K")) || (rc = check_align(fn, packed8, 16, "packed8"))) return rc;
     return launched(fn, launch_unpack8((const uint8_t *)packed8, rows, K, out_int8, (hipStream_t)stream));
 }
+
+int fptq_set_grouped_kernel(int kernel, int splits)
+{
+    if (!set_grouped_kernel(kernel, splits)) {
+        set_error("fptq_set_grouped_kernel: kernel must be 0..12, splits 1..8");
+        return FPTQ_ERR_VALUE;
+    }
+    return FPTQ_OK;
+}
+
+int fptq_grouped_kernel(int64_t M, int64_t N, int64_t K, int64_t group) { return M < 1 || N < 1 || K < 1 || group < 1 ? FPTQ_ERR_SHAPE : 1 + grouped_kernel(M, N, K, group); }
 
 }  // extern "C"

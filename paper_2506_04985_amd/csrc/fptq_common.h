@@ -61,9 +61,10 @@ hipError_t launch_gated_quantize8(const uint16_t *gate, const uint16_t *up, int6
                                   float *scale, hipStream_t s);
 hipError_t launch_unpack8(const uint8_t *packed, int64_t rows, int64_t K, int8_t *out, hipStream_t s);
 hipError_t launch_grouped_linear(const uint8_t *x, const float *token_scale, const uint8_t *w, int64_t M, int64_t N, int64_t K, int64_t group,
-                                 const float *scales, void *y, int y_type, hipStream_t s);
+                                 const float *scales, void *y, int y_type, void *scratch, int64_t scratch_bytes, hipStream_t s);
+int64_t grouped_scratch_bytes(int64_t M, int64_t N, int64_t K, int64_t group);
 int grouped_kernel(int64_t M, int64_t N, int64_t K, int64_t group);
-bool set_grouped_kernel(int kernel);
+bool set_grouped_kernel(int kernel, int splits);
 
 void set_gemm_tile(int tile);
 void set_gemm_map(int mode);

@@ -131,6 +131,33 @@ __global__ __launch_bounds__(64 * WAVES) void grouped_few_kernel(const uint8_t *
         static_cast<uint16_t *>(y)[(int64_t)t_out * N + n_out] = bf16_rne(v);
 }
 
+// y's four channels from n on of token t, from sums of 16 * value
+constexpr int PARTIAL = 2;      // beside FPTQ_BF16 and FPTQ_F32: the sums as they are
+__device__ inline void store_four(v4f v, float scale, int t, int n, int N, void *y, int y_type)
+{
+    v *= scale * 0.0625f;
+    if (y_type == FPTQ_F32) {
+        float *const to = static_cast<float *>(y) + (int64_t)t * N + n;
+        if (n + 4 <= N) {
+            __builtin_memcpy(to, &v, 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (n + e < N) to[e] = v[e];
+        }
+    } else {
+        uint16_t *const to = static_cast<uint16_t *>(y) + (int64_t)t * N + n;
+        const uint32_t pair[2] = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        if (n + 4 <= N) {
+            __builtin_memcpy(to, pair, 8);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (n + e < N) to[e] = (uint16_t)(pair[e / 2] >> (16 * (e % 2)));
+        }
+    }
+}
+
 // ---- tiles, for more tokens than a few
 //
 // A workgroup makes BN channels x BM tokens, each of its waves TN x TM sub-tiles of 32 x 32.  A K tile of both operands and its groups' scales go from HBM to LDS
@@ -172,7 +199,7 @@ __device__ inline void in_order(std::integer_sequence<int, I...>, F f)
 template <class C>
 __global__ __launch_bounds__(C::THREADS, 2) void grouped_tile_kernel(const uint8_t *__restrict__ x, const uint8_t *__restrict__ w, const float *__restrict__ scales, int M, int N,
                                                                      int ktiles, int tiles_m, int tiles_n, uint32_t tiles_per_group, uint32_t reciprocal_of_it, int groups,
-                                                                     const float *__restrict__ token_scale, void *__restrict__ y, int y_type)
+                                                                     const float *__restrict__ token_scale, void *__restrict__ y, int y_type, int split_tiles)
 {
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave_all = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -181,8 +208,9 @@ __global__ __launch_bounds__(C::THREADS, 2) void grouped_tile_kernel(const uint8
     uint8_t *const ring = lds + kg * C::RING_BYTES;
 
     // Workgroups go round the 8 XCDs; each gets a contiguous run of tiles, in bands of 8 along n, so that tiles that run together share operands in its L2.
-    const int total = tiles_m * tiles_n;
-    int pid = blockIdx.x;
+    // y_type PARTIAL: workgroup (split, tile), tiles fastest, takes K tiles split_tiles * split ... and leaves its sums in y as fp32 [splits][M][N rounded up to 4].
+    const int total = tiles_m * tiles_n, split = y_type == PARTIAL ? (int)blockIdx.x / total : 0, kt0 = split * split_tiles, kt1 = min(ktiles, kt0 + split_tiles);
+    int pid = (int)blockIdx.x - split * total;
     {
         const int per = (total + 7) / 8, tall = total % 8 == 0 ? 8 : total % 8, xcd = pid % 8, local = pid / 8;
         pid = xcd < tall ? xcd * per + local : tall * per + (xcd - tall) * (per - 1) + local;
@@ -197,10 +225,10 @@ __global__ __launch_bounds__(C::THREADS, 2) void grouped_tile_kernel(const uint8
     const int x_bytes = min(C::BM, M - m0) * KT, w_bytes = min(C::BN, N - n0) * SEG, s_bytes = min(C::BN, N - n0) * 4;
     const int x_even = wave * C::X_LOADS * 1024 + (lane >> 3) * KT, w_voff = wave * C::W_LOADS * 1024 + (lane >> 2) * SEG + (((lane & 3) ^ ((lane >> 4) & 3)) << 4);
     // the fills come in order, so that an addition makes the next addresses
-    const uint8_t *x_next = x0 + kg * x_slab, *w_next = w0 + kg * w_slab;
-    int kt_next = kg;
+    const uint8_t *x_next = x0 + (kt0 + kg) * x_slab, *w_next = w0 + (kt0 + kg) * w_slab;
+    int kt_next = kt0 + kg;
     auto next_fill = [&](int stage, Fill &f) {
-        f.live = kt_next < ktiles;
+        f.live = kt_next < kt1;
         f.x = __builtin_amdgcn_make_buffer_rsrc((void *)x_next, 0, f.live ? x_bytes : 0, RSRC_FLAGS);
         f.w = __builtin_amdgcn_make_buffer_rsrc((void *)w_next, 0, f.live ? w_bytes : 0, RSRC_FLAGS);
         uint32_t first, rest;
@@ -239,7 +267,7 @@ __global__ __launch_bounds__(C::THREADS, 2) void grouped_tile_kernel(const uint8
     v16i acc[2] = {};
     v4i xo[C::SETS][4], wo[C::TN][4], raw[C::TN][2];
     float sc[C::TN][C::GT], sc_last = 0.0f;
-    const int steps = (ktiles + C::KS - 1) / C::KS;      // the same for all sets: they share the barriers
+    const int steps = (kt1 - kt0 + C::KS - 1) / C::KS;      // the same for all sets: they share the barriers
 #pragma unroll
     for (int s = 0; s < C::STAGES - 1; ++s) {
         Fill f;
@@ -349,30 +377,27 @@ __global__ __launch_bounds__(C::THREADS, 2) void grouped_tile_kernel(const uint8
             v4f v = *reinterpret_cast<const v4f *>(out + at);
 #pragma unroll
             for (int k = 1; k < C::KS; ++k) v += *reinterpret_cast<const v4f *>(out + k * SET + at);
-            const float ts = token_scale[t] * 0.0625f;
-            v *= ts;
-            if (y_type == FPTQ_F32) {
-                float *const to = static_cast<float *>(y) + (int64_t)t * N + n;
-                if (n + 4 <= N) {
-                    __builtin_memcpy(to, &v, 16);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 3; ++e)
-                        if (n + e < N) to[e] = v[e];
-                }
-            } else {
-                uint16_t *const to = static_cast<uint16_t *>(y) + (int64_t)t * N + n;
-                const uint32_t pair[2] = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-                if (n + 4 <= N) {
-                    __builtin_memcpy(to, pair, 8);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 3; ++e)
-                        if (n + e < N) to[e] = (uint16_t)(pair[e / 2] >> (16 * (e % 2)));
-                }
+            if (y_type == PARTIAL) {
+                const int64_t stride = (N + 3) / 4 * 4;
+                *reinterpret_cast<v4f *>(static_cast<float *>(y) + ((int64_t)split * M + t) * stride + n) = v;
+                continue;
             }
+            store_four(v, token_scale[t], t, n, N, y, y_type);
         }
     }
+}
+
+// The sums of all splits of a problem, in order; a thread takes four channels of a token.
+__global__ __launch_bounds__(256) void grouped_join_kernel(const float *__restrict__ parts, int splits, int M, int N, const float *__restrict__ token_scale, void *__restrict__ y,
+                                                           int y_type)
+{
+    const int pieces = (N + 3) / 4;
+    const int64_t total = (int64_t)M * pieces, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= total) return;
+    const int t = (int)(i / pieces), n = (int)(i % pieces) * 4;
+    v4f v = *reinterpret_cast<const v4f *>(parts + i * 4);
+    for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const v4f *>(parts + (s * total + i) * 4);
+    store_four(v, token_scale[t], t, n, N, y, y_type);
 }
 
 // ---- which kernel
@@ -394,6 +419,7 @@ constexpr TileCost COSTS[] = {
     {64, 64, 4, 1, 1.15f, {2.81f}, {0.74f}},
     {64, 32, 8, 1, 0.93f, {2.16f}, {0.77f}},
 };
+constexpr float JOIN_START = 3.0f, JOIN_BYTE = 0.4e-6f;      // us: the second launch of a split K, and a byte of its ranges' sums, written and read
 template <int GT> using Tile0 = Tile<4, 2, 2, 4, 3, 1, GT>;
 template <int GT> using Tile1 = Tile<4, 2, 2, 3, 3, 1, GT>;
 template <int GT> using Tile2 = Tile<4, 1, 2, 2, 3, 2, GT>;
@@ -405,9 +431,11 @@ template <int GT> using Tile7 = Tile<1, 1, 2, 1, 2, 8, GT>;
 // groups of 32: the first would spill, the third has no room for its scales in LDS
 constexpr bool tile_serves(int i, int gt) { return gt < 4 || (i != 0 && i != 2); }
 
-static float tile_estimate(const TileCost &c, int64_t M, int64_t N, int64_t kt, int64_t cus, int gt)
+static int64_t tiles_of(const TileCost &c, int64_t M, int64_t N) { return ((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn); }
+
+static float tile_estimate(const TileCost &c, int64_t workgroups, int64_t kt, int64_t cus, int gt)
 {
-    const int64_t each = (((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn) + cus - 1) / cus, full = each / c.fit, rest = each % c.fit;      // workgroups of a CU
+    const int64_t each = (workgroups + cus - 1) / cus, full = each / c.fit, rest = each % c.fit;      // workgroups of a CU
     const float steps = (float)((kt + c.sets - 1) / c.sets) * (gt == 4 ? 1.8f : 1.0f);
     return c.start + (float)full * (c.fixed[c.fit - 1] + steps * c.step[c.fit - 1]) + (rest ? c.fixed[rest - 1] + steps * c.step[rest - 1] : 0.0f);
 }
@@ -425,29 +453,41 @@ static float few_estimate(const FewCost &c, int64_t M, int64_t N, int64_t kt, in
     return c.start + steps * (c.each * n > c.latency ? c.each * n : c.latency);
 }
 
-// The kernel of a call: 0 .. 7 a tile, 8 + i the few-token kernel FEW_COSTS[i].  Up to 16 tokens, on 10188 matrices of up to 130000 channels with groups of 128 and 64, by two lines:
+// What a call takes: 0 .. 7 a tile, 8 + i the few-token kernel FEW_COSTS[i]; into how many ranges K is split between workgroups.
+struct Choice {
+    int kernel, splits;
+};
+
+// Up to 16 tokens, on 10188 matrices of up to 130000 channels with groups of 128 and 64, by two lines:
 // short K wants eight waves; as many workgroups as CUs or a few times as many want sixteen waves, with 32 channels from 16 * CUs channels on; more workgroups want eight
 // again while K is not long.  us, 16 waves of 16 channels / 16 of 32 / 8 of 16 / 8 of 32: 4096 x 14336 7.8 / 8.9 / 10.6 / 14, 6144 x 4096 5.1 / 4.6 / 4.9 / 5.2, 28672 x 4096 - / 13.2 / 13.5 / 12.3.
 // On each of a grid of sizes the choice is within 5 % of the best of the four on average.
-static int grouped_choice(int64_t M, int64_t N, int64_t K, int gt)
+static Choice grouped_choice(int64_t M, int64_t N, int64_t K, int gt, int64_t scratch)
 {
     const int64_t kt = k_tiles(K), cus = device_cus_or_default();
     if (M <= 16) {
-        if (kt < 9) return N <= 48 * cus ? 11 : 10;
-        return N <= 16 * cus ? 8 : N > 64 * cus && kt < 33 ? 10 : 9;
+        if (kt < 9) return {N <= 48 * cus ? 11 : 10, 1};
+        return {N <= 16 * cus ? 8 : N > 64 * cus && kt < 33 ? 10 : 9, 1};
     }
     // no kernel takes less than its bytes do at 5.4 TB/s; among those that come to it the larger tile reads less (32 x 28672 x 4096, fourth from last 14.4 us, last 17.0)
     const float bytes = (float)N * (float)kt * (float)(SEG + 4 * gt) + (float)M * (float)kt * (float)KT + 2.0f * (float)M * (float)N, memory = bytes / 5.4e6f;
-    int best = -1;
+    Choice best = {-1, 1};
     float least = 0.0f;
-    auto offer = [&](int i, float us) {
+    auto offer = [&](int i, int splits, float us) {
         us = us > memory ? us : memory;
-        if (best < 0 || us < least) best = i, least = us;
+        if (best.kernel < 0 || us < least) best = {i, splits}, least = us;
     };
     for (int i = 0; i < 8; ++i)
-        if (tile_serves(i, gt)) offer(i, tile_estimate(COSTS[i], M, N, kt, cus, gt));
+        if (tile_serves(i, gt)) offer(i, 1, tile_estimate(COSTS[i], tiles_of(COSTS[i], M, N), kt, cus, gt));
     if (M <= 64)
-        for (int i = 0; i < 3; ++i) offer(8 + i, few_estimate(FEW_COSTS[i], M, N, kt, cus, gt));
+        for (int i = 0; i < 3; ++i) offer(8 + i, 1, few_estimate(FEW_COSTS[i], M, N, kt, cus, gt));
+    // Few tiles and a long K: its ranges go to workgroups of their own, and a second launch adds their sums.
+    const int64_t range = M * ((N + 3) / 4 * 16);      // bytes of a range's sums
+    for (int i = 0; i < 8; ++i) {
+        const int64_t tiles = tiles_of(COSTS[i], M, N);
+        for (int splits = 2; splits <= 8 && tile_serves(i, gt) && tiles * splits <= 2 * cus && kt / splits >= 8 && splits * range <= scratch; ++splits)
+            offer(i, splits, tile_estimate(COSTS[i], tiles * splits, (kt + splits - 1) / splits, cus, gt) + JOIN_START + (float)(splits * range) * JOIN_BYTE);
+    }
     return best;
 }
 
@@ -486,18 +526,27 @@ struct GroupedCall {
     void *y;
     int y_type;
     hipStream_t stream;
+    int splits;
+    float *parts;
 };
 
 template <class C>
 static hipError_t launch_tile(const GroupedCall &c)
 {
     const int64_t tiles_m = (c.M + C::BM - 1) / C::BM, tiles_n = (c.N + C::BN - 1) / C::BN;
-    if (tiles_m * tiles_n > (int64_t)0xffffffff / C::THREADS) return hipErrorInvalidConfiguration;
+    if (tiles_m * tiles_n * c.splits > (int64_t)0xffffffff / C::THREADS) return hipErrorInvalidConfiguration;
     const DeviceInfo *info;
     const hipError_t e = device_info(&info);      // the tiles' LDS is an attribute of the kernels, set once per device
     if (e != hipSuccess) return e;
-    grouped_tile_kernel<C><<<dim3((unsigned)(tiles_m * tiles_n)), dim3(C::THREADS), C::LDS_BYTES, c.stream>>>(
-        c.x, c.w, c.scales, c.M, c.N, c.ktiles, (int)tiles_m, (int)tiles_n, c.per, reciprocal(c.per), c.groups, c.token_scale, c.y, c.y_type);
+    const bool split = c.splits > 1;
+    grouped_tile_kernel<C><<<dim3((unsigned)(tiles_m * tiles_n * c.splits)), dim3(C::THREADS), C::LDS_BYTES, c.stream>>>(
+        c.x, c.w, c.scales, c.M, c.N, c.ktiles, (int)tiles_m, (int)tiles_n, c.per, reciprocal(c.per), c.groups, c.token_scale, split ? c.parts : c.y,
+        split ? PARTIAL : c.y_type, (c.ktiles + c.splits - 1) / c.splits);
+    if (!split) return hipGetLastError();
+    const hipError_t launched = hipGetLastError();
+    if (launched != hipSuccess) return launched;
+    const int64_t pieces = (int64_t)c.M * ((c.N + 3) / 4);
+    grouped_join_kernel<<<dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, c.stream>>>(c.parts, c.splits, c.M, c.N, c.token_scale, c.y, c.y_type);
     return hipGetLastError();
 }
 
@@ -533,27 +582,38 @@ static hipError_t launch_choice(int choice, const GroupedCall &c)
     return hipErrorInvalidValue;
 }
 
-// 0: chosen per problem; 1 + i forces choice i (testing and tuning)
+// 0: chosen per problem; 1 + i forces kernel i, in as many ranges of K as splits says where there is scratch (testing and tuning)
 static std::atomic<int> g_forced_grouped{0};
-bool set_grouped_kernel(int kernel)
+bool set_grouped_kernel(int kernel, int splits)
 {
-    if (kernel < 0 || kernel > 12) return false;
-    g_forced_grouped.store(kernel, std::memory_order_relaxed);
+    if (kernel < 0 || kernel > 12 || splits < 1 || splits > 8) return false;
+    g_forced_grouped.store(kernel + 16 * splits, std::memory_order_relaxed);
     return true;
 }
-int grouped_kernel(int64_t M, int64_t N, int64_t K, int64_t group)
+
+static Choice chosen(int64_t M, int64_t N, int64_t K, int64_t group, int64_t scratch)
 {
-    const int forced = g_forced_grouped.load(std::memory_order_relaxed);
-    return forced ? forced - 1 : grouped_choice(M, N, K, group == 32 ? 4 : group == 64 ? 2 : 1);
+    const int code = g_forced_grouped.load(std::memory_order_relaxed), forced = code % 16, splits = code / 16;
+    if (!forced) return grouped_choice(M, N, K, group == 32 ? 4 : group == 64 ? 2 : 1, scratch);
+    const bool room = forced <= 8 && splits <= k_tiles(K) && splits * M * ((N + 3) / 4 * 16) <= scratch;
+    return {forced - 1, room ? splits : 1};
 }
 
+constexpr int64_t MOST_SCRATCH = (int64_t)64 << 20;
+int64_t grouped_scratch_bytes(int64_t M, int64_t N, int64_t K, int64_t group)
+{
+    const Choice c = chosen(M, N, K, group, MOST_SCRATCH);
+    return c.splits > 1 ? c.splits * M * ((N + 3) / 4 * 16) : 0;
+}
+int grouped_kernel(int64_t M, int64_t N, int64_t K, int64_t group) { return chosen(M, N, K, group, 0).kernel; }
+
 hipError_t launch_grouped_linear(const uint8_t *x, const float *token_scale, const uint8_t *w, int64_t M, int64_t N, int64_t K, int64_t group, const float *scales,
-                                 void *y, int y_type, hipStream_t s)
+                                 void *y, int y_type, void *scratch, int64_t scratch_bytes, hipStream_t s)
 {
     const int64_t kt = k_tiles(K), per = group > KT ? (group / KT < kt ? group / KT : kt) : 1;
-    const GroupedCall c = {x, token_scale, w, (int)M, (int)N, (int)kt, (int)((K + group - 1) / group), (uint32_t)per, scales, y, y_type, s};
-    const int choice = grouped_kernel(M, N, K, group);
-    return group == 32 ? launch_choice<4>(choice, c) : group == 64 ? launch_choice<2>(choice, c) : launch_choice<1>(choice, c);
+    const Choice choice = chosen(M, N, K, group, scratch ? (scratch_bytes < MOST_SCRATCH ? scratch_bytes : MOST_SCRATCH) : 0);
+    const GroupedCall c = {x, token_scale, w, (int)M, (int)N, (int)kt, (int)((K + group - 1) / group), (uint32_t)per, scales, y, y_type, s, choice.splits, (float *)scratch};
+    return group == 32 ? launch_choice<4>(choice.kernel, c) : group == 64 ? launch_choice<2>(choice.kernel, c) : launch_choice<1>(choice.kernel, c);
 }
 
 }  // namespace fptq

@@ -519,20 +519,29 @@ PyObject *gated_quantize8(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// (xq8, token_scale, wq, M, N, K, group, w_scales, out, fp32)
+// (xq8, token_scale, wq, M, N, K, group, w_scales, out, fp32, scratch)
 PyObject *w4a8_linear(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    return guarded(n, 10, [&]() -> PyObject * {
+    return guarded(n, 11, [&]() -> PyObject * {
         const at::Tensor &xq = input(a[0], at::kChar), &s = input(a[1], at::kFloat), &wq = input(a[2], at::kByte), &w_scales = input(a[7], at::kFloat);
         const int64_t M = integer(a[3]), N = integer(a[4]), K = integer(a[5]), group = integer(a[6]);
         if (M < 1 || N < 1 || K < 1 || group < 1 || M > (1ll << 40) / K || N > (1ll << 40) / K || M > (1ll << 40) / N) throw Slow();
         if (xq.numel() < need8(M, K) || s.numel() < M || wq.numel() < need(N, K) || w_scales.numel() < ((K - 1) / group + 1) * N) throw Slow();
         const bool fp32 = truth(a[9]);
-        Output y = checked(a[8], {M, N}, fp32 ? at::kFloat : at::kBFloat16, xq);
-        void *const st = where().stream;
-        launch({&y}, [&] {
+        Output y = checked(a[8], {M, N}, fp32 ? at::kFloat : at::kBFloat16, xq), room;
+        const Where w = where();
+        void *const st = w.stream;
+        if (a[10] != Py_None) {
+            input(a[10], at::kByte);
+            room = Output(a[10], {}, at::kByte, xq);
+        } else if (M > 16 && xq.device().index() == w.device) {      // handed back when the call returns: it has to come from the stream of the launch
+            const int64_t bytes = without_gil([&] { return fptq_w4a8_linear_scratch_bytes(M, N, K, group); });
+            if (bytes < 0) throw Slow();
+            if (bytes > 0) room = Output(Py_None, {bytes}, at::kByte, xq);
+        }
+        launch({&y, &room}, [&] {
             return fptq_w4a8_linear(xq.data_ptr(), (const float *)s.data_ptr(), wq.data_ptr(), M, N, K, group, (const float *)w_scales.data_ptr(), y.ptr,
-                                    fp32 ? FPTQ_F32 : FPTQ_BF16, st);
+                                    fp32 ? FPTQ_F32 : FPTQ_BF16, room.ptr, room.numel, st);
         });
         return y.take();
     });

@@ -48,6 +48,7 @@ constexpr int SILU_FIRST = (127 - 14) << 7, SILU_COUNT = 21 << 7;
 struct SiluTable {
     float value[2 * SILU_COUNT];
 };
+static_assert(sizeof(SiluTable) % 1024 == 0, "whole wave loads");
 constexpr SiluTable silu_table()
 {
     SiluTable t = {};
@@ -177,29 +178,40 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR) void quantize8_kernel(co
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = WPR == 1 ? lane : (int)threadIdx.x, padded = (K + KT - 1) / KT * KT;
     const int64_t M = rows;
-    __shared__ __attribute__((aligned(16))) float table[TABLE ? 2 * SILU_COUNT : 4];
-    if (TABLE) {
-        for (int i = threadIdx.x; i < SILU_COUNT / 2; i += (int)blockDim.x) reinterpret_cast<v4u *>(table)[i] = reinterpret_cast<const v4u *>(SILU.value)[i];
-        __syncthreads();
-    }
-    int turn = 0;
-    for (int64_t t = WPR == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x; t < M; t += (int64_t)gridDim.x * (WPR == 1 ? 4 : 1), turn ^= 1) {
-        const uint16_t *arow = a + t * a_stride, *brow = KIND == PLAIN ? arow : b + t * b_stride;
-        v4u av[CH], bv[CH], gv[CH], sums[CH];
+    const int64_t t0 = WPR == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x, t_step = (int64_t)gridDim.x * (WPR == 1 ? 4 : 1);
+    v4u av[CH], bv[CH], gv[CH], sums[CH];
+    auto load = [&](int64_t t) {
+        const uint16_t *const arow = a + t * a_stride, *const brow = KIND == PLAIN ? arow : b + t * b_stride;
         if (RAGGED) {
             load_row_chunks(av, arow, h * 8, S * 8, K);
             if (KIND != PLAIN) load_row_chunks(bv, brow, h * 8, S * 8, K);
-            if (KEEP && KIND != GATED && gain) load_row_chunks(gv, gain, h * 8, S * 8, K);
         } else {
             const __amdgpu_buffer_rsrc_t ar = __builtin_amdgcn_make_buffer_rsrc((void *)arow, 0, K * 2, RSRC_FLAGS);
             const __amdgpu_buffer_rsrc_t br = __builtin_amdgcn_make_buffer_rsrc((void *)brow, 0, K * 2, RSRC_FLAGS);
-            const __amdgpu_buffer_rsrc_t gr = __builtin_amdgcn_make_buffer_rsrc((void *)gain, 0, K * 2, RSRC_FLAGS);
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
                 av[i] = __builtin_amdgcn_raw_buffer_load_b128(ar, (i * S + h) * 16, 0, 0);
                 if (KIND != PLAIN) bv[i] = __builtin_amdgcn_raw_buffer_load_b128(br, (i * S + h) * 16, 0, 0);
             }
-            if (KEEP && KIND != GATED && gain) {
+        }
+    };
+    __shared__ __attribute__((aligned(1024))) float table[TABLE ? 2 * SILU_COUNT : 4];
+    if (TABLE) {      // on its way to LDS while the first row is to the registers
+        const __amdgpu_buffer_rsrc_t tr = __builtin_amdgcn_make_buffer_rsrc((void *)SILU.value, 0, (int)sizeof SILU, RSRC_FLAGS);
+        for (int i = wave; i < (int)sizeof SILU / 1024; i += WPR == 1 ? 4 : WPR)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(tr, LDS_PTR(reinterpret_cast<uint8_t *>(table) + i * 1024), 16, i * 1024 + lane * 16, 0, 0, 0);
+        if (t0 < M) load(t0);
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+        __syncthreads();
+    }
+    int turn = 0;
+    for (int64_t t = t0; t < M; t += t_step, turn ^= 1) {
+        if (!TABLE) load(t);
+        if (KEEP && KIND != GATED && gain) {
+            if (RAGGED) {
+                load_row_chunks(gv, gain, h * 8, S * 8, K);
+            } else {
+                const __amdgpu_buffer_rsrc_t gr = __builtin_amdgcn_make_buffer_rsrc((void *)gain, 0, K * 2, RSRC_FLAGS);
 #pragma unroll
                 for (int i = 0; i < CH; ++i) gv[i] = __builtin_amdgcn_raw_buffer_load_b128(gr, (i * S + h) * 16, 0, 0);
             }
@@ -226,6 +238,7 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR) void quantize8_kernel(co
                 largest = largest_of(largest, scaled);
             }
         }
+        if (TABLE && t + t_step < M) load(t + t_step);
         largest = wave_max(largest);
         if (KIND != GATED && rms) ss = wave_sum(ss);
         if (WPR > 1) {
@@ -380,7 +393,8 @@ static hipError_t launch(const uint16_t *a, const uint16_t *b, const uint16_t *g
             if (K <= 2048) FPTQ_ROWS(4, 1, true);
             if (K <= 4096 && M <= 1024) FPTQ_ROWS(8, 1, true);
             if (K <= 4096) FPTQ_ROWS(4, 2, true);
-            if (K <= 8192 && M <= 512) FPTQ_ROWS(16, 1, true);
+            if (K <= 8192 && M <= 256) FPTQ_ROWS(16, 1, true);
+            if (K <= 8192 && M <= 1024) FPTQ_ROWS(8, 2, true);
             if (K > 12288 && K <= 16384 && M > 256) FPTQ_ROWS(8, 4, true);
         }
         if (K <= 6144) FPTQ_ROWS(4, 3, true);

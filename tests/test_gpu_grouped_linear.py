@@ -30,9 +30,9 @@ def tolerance(y, mass, K, group, bf16):
     return 1.01 * ((terms + 18) * 2.0 ** -24 * mass + (2.0 ** -8 * np.abs(y) if bf16 else 0)) + 1e-37
 
 
-def run(codes, s, w, ws, group, dtype=torch.float32, out=None):
+def run(codes, s, w, ws, group, dtype=torch.float32, out=None, scratch=None):
     (M, K), N = codes.shape, w.shape[0]
-    return fptq.fptq_w4a8_linear(dev(grouped.lay_out(codes)), dev(s), fptq.fptq_pack_weights(dev(w)), M, N, K, group, dev(ws), out=out, out_dtype=dtype)
+    return fptq.fptq_w4a8_linear(dev(grouped.lay_out(codes)), dev(s), fptq.fptq_pack_weights(dev(w)), M, N, K, group, dev(ws), out=out, out_dtype=dtype, scratch=scratch)
 
 
 def check(got, y, mass, K, group):
@@ -83,6 +83,24 @@ def test_every_kernel(kernel, group, forced):
             continue
         check(run(*case, group), y, mass, K, group)
         check(run(*case, group, torch.bfloat16), y, mass, K, group)
+
+
+@pytest.mark.parametrize("splits", [2, 3, 8])
+@pytest.mark.parametrize("kernel,group", [(k, g) for k in range(1, 9) for g in (32, 64, 128, 256) if g != 32 or k not in (1, 3)])
+def test_ranges_of_k(kernel, group, splits, forced):
+    """K cut between workgroups: ranges of several K tiles, of one, and without any; a caller's scratch, more than needed and full of NaN."""
+    for M, N, K in ((70, 90, 100), (33, 257, 1100), (257, 129, 2600)):
+        case = draw(M, N, K, group, kernel)
+        y, mass = grouped.linear(*case[:3], group, case[3])
+        forced(kernel, splits)
+        need = fptq.fptq_w4a8_linear_scratch_bytes(M, N, K, group)
+        assert need == (splits * M * ((N + 3) // 4 * 16) if splits <= -(-K // 128) else 0)
+        got = run(*case, group)
+        check(got, y, mass, K, group)
+        check(run(*case, group, torch.bfloat16), y, mass, K, group)
+        scratch = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")
+        assert torch.equal(run(*case, group, scratch=scratch), got) and bool((scratch[need:] == 255).all())
+        check(run(*case, group, scratch=scratch[:256]), y, mass, K, group)          # too small: as without
 
 
 @pytest.mark.parametrize("M", [1, 40, 300])

@@ -21,7 +21,7 @@ def refused(name, arguments, order, code, **changed):
 
 NORM = dict(x=P, residual=P, gain=P, M=4, K=300, mode=1, eps=1e-5, out=P, nbytes=4 * 384, scale=P, z=P, stream=None)
 GATED = dict(gate=P, up=P, M=4, K=300, gs=600, us=600, out=P, nbytes=4 * 384, scale=P, stream=None)
-LINEAR = dict(x=P, s=P, w=P, M=4, N=5, K=300, group=64, ws=P, y=P, type=0, stream=None)
+LINEAR = dict(x=P, s=P, w=P, M=4, N=5, K=300, group=64, ws=P, y=P, type=0, scratch=None, sbytes=0, stream=None)
 
 
 @pytest.mark.parametrize("code,changed", [
@@ -45,7 +45,8 @@ def test_gated(code, changed):
     (NULL, dict(x=None)), (NULL, dict(s=None)), (NULL, dict(w=None)), (NULL, dict(ws=None)), (NULL, dict(y=None)),
     (SHAPE, dict(M=0)), (SHAPE, dict(N=0)), (SHAPE, dict(K=0)), (SHAPE, dict(M=1 << 25)), (SHAPE, dict(N=(1 << 24) + 1)), (SHAPE, dict(K=1 << 25)), (SHAPE, dict(M=1 << 24, N=1 << 14)),
     (SHAPE, dict(group=0)), (SHAPE, dict(group=-128)), (SHAPE, dict(group=16)), (SHAPE, dict(group=96)), (SHAPE, dict(group=130)), (SHAPE, dict(group=192)),
-    (MODE, dict(type=2)), (MODE, dict(type=-1)), (ALIGN, dict(x=EIGHT)), (ALIGN, dict(w=EIGHT)), (ALIGN, dict(y=EIGHT)), (ALIGN, dict(s=TWO)), (ALIGN, dict(ws=TWO))])
+    (MODE, dict(type=2)), (MODE, dict(type=-1)), (ALIGN, dict(x=EIGHT)), (ALIGN, dict(w=EIGHT)), (ALIGN, dict(y=EIGHT)), (ALIGN, dict(s=TWO)), (ALIGN, dict(ws=TWO)),
+    (SIZE, dict(sbytes=-1)), (ALIGN, dict(scratch=EIGHT, sbytes=1 << 20))])
 def test_linear(code, changed):
     refused("fptq_w4a8_linear", LINEAR, list(LINEAR), code, **changed)
 
@@ -61,8 +62,11 @@ def test_sizes_and_unpack():
 def test_kernel_choice_is_host_arithmetic():
     """On 256 CUs: a few-token kernel up to 16 tokens by two lines, then the least of the fitted times."""
     L = fptq.lib()
-    for bad in (-1, 13):
-        assert L.fptq_set_grouped_kernel(bad) == VALUE
+    for bad in ((-1, 1), (13, 1), (3, 0), (3, 9)):
+        assert L.fptq_set_grouped_kernel(*bad) == VALUE
+    assert L.fptq_w4a8_linear_scratch_bytes(0, 1, 1, 128) == SHAPE and L.fptq_w4a8_linear_scratch_bytes(64, 64, 64, 100) == SHAPE
+    for M, N, K in ((1, 4096, 14336), (16, 4096, 14336), (64, 28672, 4096), (4096, 28672, 4096), (1000, 4096, 14336)):
+        assert L.fptq_w4a8_linear_scratch_bytes(M, N, K, 128) == 0
     of = L.fptq_grouped_kernel
     assert of(0, 1, 1, 32) == SHAPE and of(1, 1, 1, 0) == SHAPE
     assert of(1, 4096, 4096, 128) == 9 and of(1, 6144, 4096, 128) == 10 and of(8, 128256, 4096, 64) == 11 and of(16, 28672, 14336, 128) == 10 and of(3, 4096, 512, 128) == 12
