@@ -1,6 +1,6 @@
-"""The attention half of a decoder layer on the library's calls: quantizer, W4A4 QKV projection, rotation and paged 8-bit cache, attention,
-quantizer, W4A4 O projection.  `python -m paper_2506_04985_amd.block` runs a prompt and a token loop on random weights (a Llama-3-8B-shaped layer) and
-prints how long each takes.
+"""A decoder layer on the library's calls.  Its attention half: quantizer, W4A4 QKV projection, rotation and paged 8-bit cache, attention,
+quantizer, W4A4 O projection.  Its MLP half, with activations of 8 bits and weights of 4 bits in groups: residual and RMS norm, gate+up, gated activation, down.
+`python -m paper_2506_04985_amd.block` runs prompts and a token loop on random weights (a Llama-3-8B-shaped layer) and prints how long each takes.
 """
 import math
 
@@ -57,7 +57,28 @@ class Attention:
         return self._o(fptq.fptq_cached_attention(q, cache, table, lengths, cu))
 
 
-def main(prompt=4096, steps=64, sequences=4, heads=32, kv_heads=8, head_dim=128, width=4096):
+class Mlp:
+    """w_gate_up int8 [2 F, K] (gate's rows, then up's) and w_down int8 [N, F] in [-8, 7], with fp32 scales [ceil(K / group), 2 F] and [ceil(F / group), N] of groups of `group`
+    values of a row; gain bf16 [K] of the norm, or None where it is folded into the weights."""
+
+    def __init__(self, w_gate_up, s_gate_up, w_down, s_down, group, gain=None, eps=1e-5):
+        self.F, self.K, self.N, self.group = w_gate_up.shape[0] // 2, w_gate_up.shape[1], w_down.shape[0], group
+        if w_gate_up.shape[0] % 2 or w_down.shape[1] != self.F:
+            raise ValueError(f"weights {tuple(w_gate_up.shape)} and {tuple(w_down.shape)} do not go together")
+        if tuple(s_gate_up.shape) != (-(-self.K // group), 2 * self.F) or tuple(s_down.shape) != (-(-self.F // group), self.N):
+            raise ValueError(f"scales {tuple(s_gate_up.shape)} and {tuple(s_down.shape)} do not go with groups of {group}")
+        self.w_gate_up, self.w_down = fptq.fptq_pack_weights(w_gate_up), fptq.fptq_pack_weights(w_down)
+        self.s_gate_up, self.s_down, self.gain, self.eps = s_gate_up, s_down, gain, eps
+
+    def __call__(self, x, residual):
+        """x bf16 [T, K], the attention half's output, and the residual stream in front of it: (bf16 [T, N], the residual stream with x in it)."""
+        codes, scale, residual = fptq.fptq_norm_quantize8(x, residual, self.gain, fptq.SCALE_RMS, self.eps)
+        h = fptq.fptq_w4a8_linear(codes, scale, self.w_gate_up, x.shape[0], 2 * self.F, self.K, self.group, self.s_gate_up)
+        codes, scale = fptq.fptq_gated_quantize8(*h.split(self.F, 1))
+        return fptq.fptq_w4a8_linear(codes, scale, self.w_down, x.shape[0], self.N, self.F, self.group, self.s_down), residual
+
+
+def main(prompt=4096, steps=64, sequences=4, heads=32, kv_heads=8, head_dim=128, width=4096, mlp_width=None, group=128):
     g = torch.Generator(device="cuda").manual_seed(0)
     weights = lambda n, k: torch.randint(-8, 8, (n, k), dtype=torch.int8, device="cuda", generator=g)
     rows = (heads + 2 * kv_heads) * head_dim
@@ -66,6 +87,10 @@ def main(prompt=4096, steps=64, sequences=4, heads=32, kv_heads=8, head_dim=128,
     s_rows = torch.full((width,), 0.01, device="cuda")
     total = prompt // sequences + steps
     layer = Attention(weights(rows, width), s_qkv, weights(width, heads * head_dim), s_rows, heads, kv_heads, head_dim, s_x, 0.05, rope_table(total, head_dim))
+    if mlp_width:
+        unit = lambda n, k: torch.full((-(-k // group), n), 1.0 / math.sqrt(21.5 * k), device="cuda")
+        mlp = Mlp(weights(2 * mlp_width, width), unit(2 * mlp_width, width), weights(width, mlp_width), unit(width, mlp_width), group,
+                  torch.ones(width, dtype=torch.bfloat16, device="cuda"))
     pages = -(-total // PAGE)
     cache = fptq.Cache.empty(sequences * pages, kv_heads, head_dim)
     table = torch.randperm(sequences * pages, device="cuda", generator=g).to(torch.int32).view(sequences, pages)
@@ -90,16 +115,20 @@ def main(prompt=4096, steps=64, sequences=4, heads=32, kv_heads=8, head_dim=128,
     layer.prompt(x, cache, table, lengths, cu)
     y, us = timed(lambda: layer.prompt(x, cache, table, lengths, cu), 10)
     print(f"prompts of {sequences} x {prompt // sequences} tokens: {us:.1f} us, output {tuple(y.shape)}, finite: {bool(torch.isfinite(y).all())}")
+    if mlp_width:
+        (y, _), us = timed(lambda: mlp(y, x), 10)
+        print(f"their MLP half: {us:.1f} us, output {tuple(y.shape)}, finite: {bool(torch.isfinite(y).all())}")
     # the token loop as a server runs it: one captured step, replayed on growing lengths
     before = lengths.clone()
-    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
-    side.wait_stream(torch.cuda.current_stream())
-    with torch.cuda.graph(graph, stream=side):
-        y = step()
-    lengths.copy_(before)
-    _, us = timed(graph.replay, steps)
-    print(f"a token of {sequences} sequences behind {prompt // sequences} to {total}: {us:.1f} us, output {tuple(y.shape)}, finite: {bool(torch.isfinite(y).all())}")
+    for what, call in [("", step)] + [(", with its MLP half", lambda: mlp(step(), token)[0])] * bool(mlp_width):
+        lengths.copy_(before)
+        graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=side):
+            y = call()
+        _, us = timed(graph.replay, steps)
+        print(f"a token of {sequences} sequences behind {prompt // sequences} to {total}{what}: {us:.1f} us, output {tuple(y.shape)}, finite: {bool(torch.isfinite(y).all())}")
 
 
 if __name__ == "__main__":
-    main()
+    main(mlp_width=14336)
