@@ -355,7 +355,7 @@ int fptq_gated_quantize8(const void *gate, const void *up, int64_t M, int64_t K,
  *   scratch      device, 256-byte aligned, at least fptq_w4a8_linear_scratch_bytes(...) bytes (64 MB at most, 0 for most shapes), or NULL.  With it a long K against few
  *                outputs is shared out to more workgroups, in two launches.  Too small: as NULL.  Its contents need no initialisation and mean nothing afterwards.
  *                Calls that share it must not overlap in time.
- * M and N up to 2^24, M * N up to 2^37.
+ * M and N up to 2^24, M * N up to 2^36.  The sums are kept 16 times as large: from 2^124 on, before the token's scale, they are infinite.
  */
 #define FPTQ_BF16 0
 #define FPTQ_F32 1

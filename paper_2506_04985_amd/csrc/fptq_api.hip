@@ -73,7 +73,7 @@ int device_cus_or_default()
 }
 
 // Tokens or channels, and outputs, of a linear call with 8-bit activations: what keeps a launch below 2^32 threads.
-static const int64_t GROUPED_MOST = (int64_t)1 << 24, GROUPED_OUTPUTS = (int64_t)1 << 37;
+static const int64_t GROUPED_MOST = (int64_t)1 << 24, GROUPED_OUTPUTS = (int64_t)1 << 36;
 
 static int check_dims(const char *fn, int64_t a, int64_t b, const char *an, const char *bn)
 {

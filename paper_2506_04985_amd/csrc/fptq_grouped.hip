@@ -163,8 +163,13 @@ __device__ inline void store_four(v4f v, float scale, int t, int n, int N, void 
 // A workgroup makes BN channels x BM tokens, each of its waves TN x TM sub-tiles of 32 x 32.  A K tile of both operands and its groups' scales go from HBM to LDS
 // by loads that write LDS directly, STAGES deep, one barrier a K tile.  v_mfma_i32_32x32x32_i8 makes a group's integer sums, which go into the fp32 sums at once: with tokens
 // as rows of the result and channels as columns a lane has one channel of a sub-tile, so its scale is one register, and (float)sum and a fused multiply-add are the 32
-// vector instructions that 4 MFMAs (128 cycles) of a 128-value group cost.  Two waves a SIMD, so that one's conversions run under the other's MFMAs.
-// KS sets of WAVES waves share the tile, set g taking K tiles g, g + KS, ... through a ring of its own; with one wave in a set nobody waits for another before the end.
+// vector instructions that the 4 MFMAs of a 128-value group cost.  KS sets of WAVES waves share the tile, set g taking K tiles g, g + KS, ... through a ring of its own; with one wave in a set
+// nobody waits for another before the end.
+//
+// What bounds the large tiles: those conversions beside the MFMAs, then power.  An MFMA takes 33.5 cycles alone, with four conversions and four multiply-adds behind it 51 (two waves a SIMD,
+// measured in registers); 256 x 256 walks a K tile in 1.50 us on zeros, 56 cycles an MFMA, and in 1.9 on dense operands, where the clock falls to 1.75 GHz (4096 x 28672 x 4096 485 to 515 us, 1.9 to
+// 2.0 POP/s; MFMAs busy in 45 % of the cycles).  Two waves a SIMD, so that one's conversions run under the other's MFMAs; within a wave they are pinned behind the MFMAs of the next
+// unit, without which that launch took 539 us on a card where it now takes 514.
 typedef int v16i __attribute__((ext_vector_type(16)));
 
 template <int WAVES_N_, int WAVES_M_, int TN_, int TM_, int STAGES_, int KS_, int GT_>
@@ -402,9 +407,10 @@ __global__ __launch_bounds__(256) void grouped_join_kernel(const float *__restri
 
 // ---- which kernel
 //
-// What a tile shape's launch takes, in us, fitted on 2288 launches of random sizes (17 to 6000 tokens, 256 to 60000 channels, K up to 16384, groups of 128 and
-// more, weights not in any cache) on an MI355X: `start`, and for every CU, FIT workgroups at a time, `fixed` and `step` a K tile of a set, which depend on how many run there
-// together.  With groups of 64 the same choice is within 1 % of the best on average, with groups of 32 a step takes about 1.8 times as long.
+// What a tile shape's launch takes, in us, fitted on 2928 problems of random sizes (17 to 6000 tokens, 256 to 60000 channels, K up to 16384, groups of 128, weights not in any cache), each
+// run with every shape on an MI355X: `start`, and for every CU, `fit` workgroups at a time, `fixed` and `step` a K tile of a set, which depend on how many run there
+// together.  Against the best of 14 shapes and five few-token kernels the choice takes 1.4 to 2.2 % longer on average and 9 to 12 % at the 95th percentile; with groups of 64 (1287 problems) 0.7 to
+// 1.8 and 6 to 11 %, with groups of 32 (1340), where a step takes about 1.8 times as long, 2.0 to 4.7 and 11 to 24 %.
 struct TileCost {
     int bn, bm, sets, fit;
     float start, fixed[3], step[3];
@@ -461,7 +467,7 @@ struct Choice {
 // Up to 16 tokens, on 10188 matrices of up to 130000 channels with groups of 128 and 64, by two lines:
 // short K wants eight waves; as many workgroups as CUs or a few times as many want sixteen waves, with 32 channels from 16 * CUs channels on; more workgroups want eight
 // again while K is not long.  us, 16 waves of 16 channels / 16 of 32 / 8 of 16 / 8 of 32: 4096 x 14336 7.8 / 8.9 / 10.6 / 14, 6144 x 4096 5.1 / 4.6 / 4.9 / 5.2, 28672 x 4096 - / 13.2 / 13.5 / 12.3.
-// On each of a grid of sizes the choice is within 5 % of the best of the four on average.
+// The choice takes 0.3 to 1.5 % longer than the best kernel on average.
 static Choice grouped_choice(int64_t M, int64_t N, int64_t K, int gt, int64_t scratch)
 {
     const int64_t kt = k_tiles(K), cus = device_cus_or_default();

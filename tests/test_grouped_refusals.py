@@ -43,7 +43,7 @@ def test_gated(code, changed):
 
 @pytest.mark.parametrize("code,changed", [
     (NULL, dict(x=None)), (NULL, dict(s=None)), (NULL, dict(w=None)), (NULL, dict(ws=None)), (NULL, dict(y=None)),
-    (SHAPE, dict(M=0)), (SHAPE, dict(N=0)), (SHAPE, dict(K=0)), (SHAPE, dict(M=1 << 25)), (SHAPE, dict(N=(1 << 24) + 1)), (SHAPE, dict(K=1 << 25)), (SHAPE, dict(M=1 << 24, N=1 << 14)),
+    (SHAPE, dict(M=0)), (SHAPE, dict(N=0)), (SHAPE, dict(K=0)), (SHAPE, dict(M=1 << 25)), (SHAPE, dict(N=(1 << 24) + 1)), (SHAPE, dict(K=1 << 25)), (SHAPE, dict(M=1 << 24, N=(1 << 12) + 1)),
     (SHAPE, dict(group=0)), (SHAPE, dict(group=-128)), (SHAPE, dict(group=16)), (SHAPE, dict(group=96)), (SHAPE, dict(group=130)), (SHAPE, dict(group=192)),
     (MODE, dict(type=2)), (MODE, dict(type=-1)), (ALIGN, dict(x=EIGHT)), (ALIGN, dict(w=EIGHT)), (ALIGN, dict(y=EIGHT)), (ALIGN, dict(s=TWO)), (ALIGN, dict(ws=TWO)),
     (SIZE, dict(sbytes=-1)), (ALIGN, dict(scratch=EIGHT, sbytes=1 << 20))])
