@@ -181,7 +181,8 @@ struct Tile {
     static constexpr int LOADS = X_LOADS + W_LOADS + S_LOADS, RING_BYTES = STAGES * STAGE_BYTES;
     static constexpr int SETS = TN * TM * 16 <= 96 && TM > 1 ? 2 : 1;
     static constexpr int OUT_ROWS = WAVES_M * 32, OUT_BYTES = KS * OUT_ROWS * BN * 4;      // a pass of the epilogue
-    static constexpr int LDS_BYTES = KS * RING_BYTES > OUT_BYTES ? KS * RING_BYTES : OUT_BYTES;
+    static constexpr int PASSES = TM > 1 && 2 * OUT_BYTES <= KS * RING_BYTES ? 2 : 1;      // of them that LDS holds
+    static constexpr int SCALES_AT = KS * RING_BYTES > OUT_BYTES ? KS * RING_BYTES : OUT_BYTES, LDS_BYTES = SCALES_AT + BM * 4;      // the tokens' scales lie behind
     static_assert(X_BYTES % (WAVES * 1024) == 0 && W_BYTES % (WAVES * 1024) == 0 && BN % 64 == 0, "a K tile is shared out evenly");
     static_assert(S_PIECES % WAVES == 0 || WAVES % S_PIECES == 0, "waves without a piece of their own repeat another's");
     static_assert(LOADS * (STAGES - 1) < 64, "the count of loads in flight has six bits");
@@ -273,6 +274,13 @@ __global__ __launch_bounds__(C::THREADS, 2) void grouped_tile_kernel(const uint8
     v4i xo[C::SETS][4], wo[C::TN][4], raw[C::TN][2];
     float sc[C::TN][C::GT], sc_last = 0.0f;
     const int steps = (kt1 - kt0 + C::KS - 1) / C::KS;      // the same for all sets: they share the barriers
+    // the tokens' scales, first of all loads; waves without a piece of their own repeat another's
+    {
+        const __amdgpu_buffer_rsrc_t tr = __builtin_amdgcn_make_buffer_rsrc((void *)(token_scale + m0), 0, min(C::BM, M - m0) * 4, RSRC_FLAGS);
+        constexpr int PIECES = (C::BM + 63) / 64;
+        const int piece = wave_all % PIECES;
+        if (C::BM % 64 == 0 || lane < C::BM) __builtin_amdgcn_raw_ptr_buffer_load_lds(tr, LDS_PTR(lds + C::SCALES_AT + piece * 256), 4, (piece * 64 + lane) * 4, 0, 0, 0);
+    }
 #pragma unroll
     for (int s = 0; s < C::STAGES - 1; ++s) {
         Fill f;
@@ -364,30 +372,33 @@ __global__ __launch_bounds__(C::THREADS, 2) void grouped_tile_kernel(const uint8
     // ---- epilogue, 32 tokens of each wave at a time: the sums go to LDS as [set][token][channel] and come back four channels of a token to a thread, whose sets it
     // adds in order.  Register r of lane (i, h) is token 8 (r / 4) + 4 h + r % 4, channel i of its sub-tile.
     float *const out = reinterpret_cast<float *>(lds);
+    const float *const token_scales = reinterpret_cast<const float *>(lds + C::SCALES_AT);
     constexpr int PIECES = C::OUT_ROWS * C::BN / 4 / C::THREADS, SET = C::OUT_ROWS * C::BN;
     const int n = n0 + (tid * 4) % C::BN;
+    __syncthreads();
 #pragma unroll
     for (int tm = 0; tm < C::TM; ++tm) {
-        __syncthreads();
+        float *const pass = out + tm % C::PASSES * (C::KS * SET);
+        if (C::PASSES == 1 && tm > 0) __syncthreads();
 #pragma unroll
         for (int tn = 0; tn < C::TN; ++tn)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-                out[kg * SET + (wave_m * 32 + 8 * (r / 4) + 4 * h + r % 4) * C::BN + (wave_n * C::TN + tn) * 32 + i32] = sum[tn][tm][r];
+                pass[kg * SET + (wave_m * 32 + 8 * (r / 4) + 4 * h + r % 4) * C::BN + (wave_n * C::TN + tn) * 32 + i32] = sum[tn][tm][r];
         __syncthreads();
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
-            const int at = (p * C::THREADS + tid) * 4, row = at / C::BN, t = m0 + (row / 32 * C::TM + tm) * 32 + row % 32;
+            const int at = (p * C::THREADS + tid) * 4, row = at / C::BN, of_tile = (row / 32 * C::TM + tm) * 32 + row % 32, t = m0 + of_tile;
             if (t >= M || n >= N) continue;
-            v4f v = *reinterpret_cast<const v4f *>(out + at);
+            v4f v = *reinterpret_cast<const v4f *>(pass + at);
 #pragma unroll
-            for (int k = 1; k < C::KS; ++k) v += *reinterpret_cast<const v4f *>(out + k * SET + at);
+            for (int k = 1; k < C::KS; ++k) v += *reinterpret_cast<const v4f *>(pass + k * SET + at);
             if (y_type == PARTIAL) {
                 const int64_t stride = (N + 3) / 4 * 4;
                 *reinterpret_cast<v4f *>(static_cast<float *>(y) + ((int64_t)split * M + t) * stride + n) = v;
                 continue;
             }
-            store_four(v, token_scale[t], t, n, N, y, y_type);
+            store_four(v, token_scales[of_tile], t, n, N, y, y_type);
         }
     }
 }
