@@ -422,23 +422,45 @@ __global__ __launch_bounds__(256) void grouped_join_kernel(const float *__restri
 
 // ---- which kernel
 //
-// What a tile shape's launch takes, in us, fitted on 2928 problems of random sizes (17 to 6000 tokens, 256 to 60000 channels, K up to 16384, groups of 128, weights not in any cache), each
-// run with every shape on an MI355X: `start`, and for every CU, `fit` workgroups at a time, `fixed` and `step` a K tile of a set, which depend on how many run there
-// together.  Against the best of 14 shapes and five few-token kernels the choice takes 1.4 to 2.2 % longer on average and 9 to 12 % at the 95th percentile; with groups of 64 (1287 problems) 0.7 to
-// 1.8 and 6 to 11 %, with groups of 32 (1340), where a step takes about 1.8 times as long, 2.0 to 4.7 and 11 to 24 %.
+// What a tile shape's launch takes, in us, fitted on 5636 problems of random sizes (17 to 6000 tokens, 256 to 60000 channels, K up to 16384, weights not in any cache; 2464 of them in
+// groups of 128, 1552 in groups of 64, 1620 in groups of 32), each run with every shape on an MI355X: `start`, and for every CU, `fit` workgroups at a time, `fixed` and `step` a K tile of
+// a set, which depend on how many run there together.  Against the best of these eight and of four few-token kernels the choice takes, from 65 tokens on, 0.3 to 0.7 % longer on average
+// and 2 to 5 % at the 95th percentile, and up to 64 tokens 2.0 to 3.1 and 11 to 15 %.
 struct TileCost {
     int bn, bm, sets, fit;
     float start, fixed[3], step[3];
 };
-constexpr TileCost COSTS[] = {
-    {256, 256, 1, 1, 0.0f, {11.78f}, {1.66f}},
-    {256, 192, 1, 1, 0.0f, {9.32f}, {1.36f}},
-    {256, 64, 2, 1, 0.65f, {4.27f}, {1.13f}},
-    {128, 64, 1, 3, 3.17f, {0.81f, 1.82f, 3.26f}, {0.49f, 0.74f, 0.96f}},
-    {128, 64, 2, 1, 0.92f, {2.89f}, {0.64f}},
-    {128, 32, 2, 2, 2.12f, {0.76f, 2.26f}, {0.56f, 0.79f}},
-    {64, 64, 4, 1, 1.15f, {2.81f}, {0.74f}},
-    {64, 32, 8, 1, 0.93f, {2.16f}, {0.77f}},
+constexpr TileCost COSTS[3][8] = {      // groups of 128 and more, of 64, of 32 (zeros: no such kernel)
+    {
+        {256, 256, 1, 1, 0.00f, {9.05f}, {1.60f}},
+        {256, 192, 1, 1, 0.39f, {7.07f}, {1.34f}},
+        {256, 64, 2, 1, 1.17f, {3.79f}, {1.10f}},
+        {128, 64, 1, 3, 2.79f, {1.01f, 1.87f, 2.62f}, {0.49f, 0.72f, 0.96f}},
+        {128, 64, 2, 1, 1.30f, {2.69f}, {0.62f}},
+        {128, 32, 2, 2, 2.52f, {1.05f, 2.05f}, {0.55f, 0.76f}},
+        {64, 64, 4, 1, 1.31f, {2.90f}, {0.74f}},
+        {64, 32, 8, 1, 1.43f, {2.00f}, {0.78f}},
+    },
+    {
+        {256, 256, 1, 1, 0.18f, {8.95f}, {2.25f}},
+        {256, 192, 1, 1, 0.89f, {6.93f}, {1.78f}},
+        {256, 64, 2, 1, 1.30f, {3.82f}, {1.38f}},
+        {128, 64, 1, 3, 2.95f, {0.81f, 1.72f, 2.60f}, {0.57f, 0.83f, 1.13f}},
+        {128, 64, 2, 1, 1.34f, {2.67f}, {0.78f}},
+        {128, 32, 2, 2, 2.57f, {1.05f, 2.13f}, {0.64f, 0.90f}},
+        {64, 64, 4, 1, 1.42f, {2.78f}, {0.94f}},
+        {64, 32, 8, 1, 1.46f, {2.00f}, {0.93f}},
+    },
+    {
+        {256, 256, 1, 1, 0.00f, {0.00f}, {0.00f}},
+        {256, 192, 1, 1, 1.00f, {6.72f}, {2.79f}},
+        {256, 64, 2, 1, 0.00f, {0.00f}, {0.00f}},
+        {128, 64, 1, 3, 3.77f, {0.00f, 0.97f, 3.55f}, {0.82f, 1.19f, 1.68f}},
+        {128, 64, 2, 1, 1.32f, {2.76f}, {1.11f}},
+        {128, 32, 2, 2, 1.79f, {1.90f, 4.42f}, {0.90f, 1.76f}},
+        {64, 64, 4, 1, 1.33f, {2.90f}, {1.41f}},
+        {64, 32, 8, 1, 1.47f, {2.01f}, {1.28f}},
+    },
 };
 constexpr float JOIN_START = 3.0f, JOIN_BYTE = 0.4e-6f;      // us: the second launch of a split K, and a byte of its ranges' sums, written and read
 template <int GT> using Tile0 = Tile<4, 2, 2, 4, 3, 1, GT>;
@@ -454,10 +476,10 @@ constexpr bool tile_serves(int i, int gt) { return gt < 4 || (i != 0 && i != 2);
 
 static int64_t tiles_of(const TileCost &c, int64_t M, int64_t N) { return ((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn); }
 
-static float tile_estimate(const TileCost &c, int64_t workgroups, int64_t kt, int64_t cus, int gt)
+static float tile_estimate(const TileCost &c, int64_t workgroups, int64_t kt, int64_t cus)
 {
     const int64_t each = (workgroups + cus - 1) / cus, full = each / c.fit, rest = each % c.fit;      // workgroups of a CU
-    const float steps = (float)((kt + c.sets - 1) / c.sets) * (gt == 4 ? 1.8f : 1.0f);
+    const float steps = (float)((kt + c.sets - 1) / c.sets);
     return c.start + (float)full * (c.fixed[c.fit - 1] + steps * c.step[c.fit - 1]) + (rest ? c.fixed[rest - 1] + steps * c.step[rest - 1] : 0.0f);
 }
 
@@ -490,8 +512,9 @@ static Choice grouped_choice(int64_t M, int64_t N, int64_t K, int gt, int64_t sc
         if (kt < 9) return {N <= 48 * cus ? 11 : 10, 1};
         return {N <= 16 * cus ? 8 : N > 64 * cus && kt < 33 ? 10 : 9, 1};
     }
-    // no kernel takes less than its bytes do at 5.4 TB/s; among those that come to it the larger tile reads less (32 x 28672 x 4096, fourth from last 14.4 us, last 17.0)
-    const float bytes = (float)N * (float)kt * (float)(SEG + 4 * gt) + (float)M * (float)kt * (float)KT + 2.0f * (float)M * (float)N, memory = bytes / 5.4e6f;
+    // no kernel takes less than its bytes do at 5.1 TB/s; among those that come to it the larger tile reads less (32 x 28672 x 4096, fourth from last 14.4 us, last 17.0)
+    const float bytes = (float)N * (float)kt * (float)(SEG + 4 * gt) + (float)M * (float)kt * (float)KT + 2.0f * (float)M * (float)N, memory = bytes / 5.1e6f;
+    const TileCost *const costs = COSTS[gt >> 1];
     Choice best = {-1, 1};
     float least = 0.0f;
     auto offer = [&](int i, int splits, float us) {
@@ -499,15 +522,15 @@ static Choice grouped_choice(int64_t M, int64_t N, int64_t K, int gt, int64_t sc
         if (best.kernel < 0 || us < least) best = {i, splits}, least = us;
     };
     for (int i = 0; i < 8; ++i)
-        if (tile_serves(i, gt)) offer(i, 1, tile_estimate(COSTS[i], tiles_of(COSTS[i], M, N), kt, cus, gt));
+        if (tile_serves(i, gt)) offer(i, 1, tile_estimate(costs[i], tiles_of(costs[i], M, N), kt, cus));
     if (M <= 64)
         for (int i = 0; i < 3; ++i) offer(8 + i, 1, few_estimate(FEW_COSTS[i], M, N, kt, cus, gt));
     // Few tiles and a long K: its ranges go to workgroups of their own, and a second launch adds their sums.
     const int64_t range = M * ((N + 3) / 4 * 16);      // bytes of a range's sums
     for (int i = 0; i < 8; ++i) {
-        const int64_t tiles = tiles_of(COSTS[i], M, N);
+        const int64_t tiles = tiles_of(costs[i], M, N);
         for (int splits = 2; splits <= 8 && tile_serves(i, gt) && tiles * splits <= 2 * cus && kt / splits >= 8 && splits * range <= scratch; ++splits)
-            offer(i, splits, tile_estimate(COSTS[i], tiles * splits, (kt + splits - 1) / splits, cus, gt) + JOIN_START + (float)(splits * range) * JOIN_BYTE);
+            offer(i, splits, tile_estimate(costs[i], tiles * splits, (kt + splits - 1) / splits, cus) + JOIN_START + (float)(splits * range) * JOIN_BYTE);
     }
     return best;
 }
