@@ -425,7 +425,7 @@ __global__ __launch_bounds__(256) void grouped_join_kernel(const float *__restri
 // What a tile shape's launch takes, in us, fitted on 5636 problems of random sizes (17 to 6000 tokens, 256 to 60000 channels, K up to 16384, weights not in any cache; 2464 of them in
 // groups of 128, 1552 in groups of 64, 1620 in groups of 32), each run with every shape on an MI355X: `start`, and for every CU, `fit` workgroups at a time, `fixed` and `step` a K tile of
 // a set, which depend on how many run there together.  Against the best of these eight and of four few-token kernels the choice takes, from 65 tokens on, 0.3 to 0.7 % longer on average
-// and 2 to 5 % at the 95th percentile, and up to 64 tokens 2.0 to 3.1 and 11 to 15 %.
+// and 2 to 5 % at the 95th percentile, and up to 64 tokens 1.4 to 1.9 and 8 to 9 %.
 struct TileCost {
     int bn, bm, sets, fit;
     float start, fixed[3], step[3];
@@ -483,20 +483,22 @@ static float tile_estimate(const TileCost &c, int64_t workgroups, int64_t kt, in
     return c.start + (float)full * (c.fixed[c.fit - 1] + steps * c.step[c.fit - 1]) + (rest ? c.fixed[rest - 1] + steps * c.step[rest - 1] : 0.0f);
 }
 
-// The few-token kernels the same way: a start, and for every K tile of a wave a latency or what the workgroups of a CU take together.
+// The few-token kernels the same way: a start, and for every K tile of a wave a latency and what each workgroup of a CU adds.
 struct FewCost {
     int waves, channels;
     float start, latency, each;
 };
-constexpr FewCost FEW_COSTS[] = {{16, 16, 2.07f, 0.70f, 0.87f}, {16, 32, 1.96f, 0.98f, 1.27f}, {8, 32, 2.15f, 0.68f, 0.71f}, {8, 16, 0.0f, 0.0f, 0.0f}};
+constexpr FewCost FEW_COSTS[3][3] = {{{16, 16, 1.82f, 0.37f, 0.79f}, {16, 32, 1.52f, 0.57f, 1.10f}, {8, 32, 2.27f, 0.14f, 0.62f}},
+                                     {{16, 16, 1.74f, 0.34f, 0.90f}, {16, 32, 1.62f, 0.59f, 1.08f}, {8, 32, 2.35f, 0.12f, 0.67f}},
+                                     {{16, 16, 0.85f, 1.27f, 1.07f}, {16, 32, 0.90f, 1.33f, 1.38f}, {8, 32, 2.12f, 0.38f, 0.87f}}};
 
-static float few_estimate(const FewCost &c, int64_t M, int64_t N, int64_t kt, int64_t cus, int gt)
+static float few_estimate(const FewCost &c, int64_t M, int64_t N, int64_t kt, int64_t cus)
 {
-    const float steps = (float)((kt + c.waves - 1) / c.waves) * (gt == 4 ? 1.5f : 1.0f), n = (float)((N + c.channels - 1) / c.channels * ((M + 15) / 16)) / (float)cus;
-    return c.start + steps * (c.each * n > c.latency ? c.each * n : c.latency);
+    const int64_t steps = (kt + c.waves - 1) / c.waves, each = ((N + c.channels - 1) / c.channels * ((M + 15) / 16) + cus - 1) / cus;
+    return c.start + (float)steps * (c.latency + (float)each * c.each);
 }
 
-// What a call takes: 0 .. 7 a tile, 8 + i the few-token kernel FEW_COSTS[i]; into how many ranges K is split between workgroups.
+// What a call takes: 0 .. 7 a tile, 8 + i the few-token kernel FEW_COSTS[..][i], 11 the one of eight waves and 16 channels; into how many ranges K is split between workgroups.
 struct Choice {
     int kernel, splits;
 };
@@ -504,11 +506,14 @@ struct Choice {
 // Up to 16 tokens, on 10188 matrices of up to 130000 channels with groups of 128 and 64, by two lines:
 // short K wants eight waves; as many workgroups as CUs or a few times as many want sixteen waves, with 32 channels from 16 * CUs channels on; more workgroups want eight
 // again while K is not long.  us, 16 waves of 16 channels / 16 of 32 / 8 of 16 / 8 of 32: 4096 x 14336 7.8 / 8.9 / 10.6 / 14, 6144 x 4096 5.1 / 4.6 / 4.9 / 5.2, 28672 x 4096 - / 13.2 / 13.5 / 12.3.
-// The choice takes 0.3 to 1.5 % longer than the best kernel on average.
+// From 13 tokens on such a kernel reads as many bytes of tokens as of weights, and a long K against many channels wants tiles (sixteen waves of
+// 32 channels / tile: 15 x 9600 x 13952 24.0 / 20.0, 16 x 30656 x 14080 55.3 / 46.3).  The choice takes 0.3 to 1.5 % longer than the best kernel on average, with 13 to 16 tokens and more than 64M weights 2 to 4 %.
 static Choice grouped_choice(int64_t M, int64_t N, int64_t K, int gt, int64_t scratch)
 {
     const int64_t kt = k_tiles(K), cus = device_cus_or_default();
     if (M <= 16) {
+        if (M > 12 && kt >= 32 && N > 32 * cus && N <= 64 * cus) return {7, 1};
+        if (M > 12 && kt >= 48 && N > 96 * cus) return {gt == 4 ? 7 : 5, 1};
         if (kt < 9) return {N <= 48 * cus ? 11 : 10, 1};
         return {N <= 16 * cus ? 8 : N > 64 * cus && kt < 33 ? 10 : 9, 1};
     }
@@ -524,7 +529,7 @@ static Choice grouped_choice(int64_t M, int64_t N, int64_t K, int gt, int64_t sc
     for (int i = 0; i < 8; ++i)
         if (tile_serves(i, gt)) offer(i, 1, tile_estimate(costs[i], tiles_of(costs[i], M, N), kt, cus));
     if (M <= 64)
-        for (int i = 0; i < 3; ++i) offer(8 + i, 1, few_estimate(FEW_COSTS[i], M, N, kt, cus, gt));
+        for (int i = 0; i < 3; ++i) offer(8 + i, 1, few_estimate(FEW_COSTS[gt >> 1][i], M, N, kt, cus));
     // Few tiles and a long K: its ranges go to workgroups of their own, and a second launch adds their sums.
     const int64_t range = M * ((N + 3) / 4 * 16);      // bytes of a range's sums
     for (int i = 0; i < 8; ++i) {

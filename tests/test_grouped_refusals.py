@@ -69,7 +69,7 @@ def test_kernel_choice_is_host_arithmetic():
         assert L.fptq_w4a8_linear_scratch_bytes(M, N, K, 128) == 0
     of = L.fptq_grouped_kernel
     assert of(0, 1, 1, 32) == SHAPE and of(1, 1, 1, 0) == SHAPE
-    assert of(1, 4096, 4096, 128) == 9 and of(1, 6144, 4096, 128) == 10 and of(8, 128256, 4096, 64) == 11 and of(16, 28672, 14336, 128) == 10 and of(3, 4096, 512, 128) == 12
+    assert of(1, 4096, 4096, 128) == 9 and of(1, 6144, 4096, 128) == 10 and of(8, 128256, 4096, 64) == 11 and of(12, 28672, 14336, 128) == 10 and of(16, 28672, 14336, 128) == 6 and of(16, 28672, 14336, 32) == 8 and of(3, 4096, 512, 128) == 12
     assert of(4096, 28672, 4096, 128) == 1 and of(333, 32003, 2504, 64) == 2 and of(1000, 4096, 14336, 128) == 3 and of(32, 28672, 4096, 128) == 6
     for M in (17, 64, 65, 500, 3000):
         for N in (64, 1000, 5000, 40000):
