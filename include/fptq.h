@@ -329,7 +329,8 @@ int64_t fptq_packed8_bytes(int64_t rows, int64_t K);
  *   x_bf16        device, bf16 [M x K]
  *   residual      device, bf16 [M x K], or NULL: z = x
  *   gain          device, bf16 [K], or NULL: u = z
- *   scale_mode    FPTQ_SCALE_RMS: inv = (float)(1 / sqrt(sum z^2 / K + eps)), the sum in fp64; FPTQ_SCALE_NONE: inv = 1
+ *   scale_mode    FPTQ_SCALE_RMS: inv = (float)(1 / sqrt(sum z^2 / K + eps)), the sum in fp64 (eps = 0: infinite for a row
+ *                 below 2^-128, whose scale is then infinite as well, but 0 for a row of zeros); FPTQ_SCALE_NONE: inv = 1
  *   residual_out  device, bf16 [M x K], or NULL; needs residual, and may be it or x_bf16
  * The norm's factor is one for a row, so the codes do not depend on it.
  */
@@ -346,7 +347,7 @@ int fptq_gated_quantize8(const void *gate, const void *up, int64_t M, int64_t K,
 
 /*
  * y[t, n] = token_scale[t] * sum_g w_scales[g, n] * (sum over the group's k of code[t, k] * w[n, k]), from one token to long prompts.
- * The inner sums are exact integers; those of the groups are added in fp32, in an order that the shape and the scratch alone decide.
+ * Sums over a group's values, or over 128 of them where it has more, are exact integers; they are added in fp32, in an order that the shape and the scratch alone decide.
  *   xq8          device, codes from one of the quantizers above
  *   w_packed     device, packed weights [N x K] from fptq_pack_weights
  *   group        values of K to a scale: 32, 64 or a multiple of 128 (of K or more: one scale a channel); the last group may be shorter

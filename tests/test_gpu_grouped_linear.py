@@ -149,6 +149,23 @@ def test_nothing_is_written_behind_the_last_row(M, N, K, group, dtype):
     assert bool((whole[M * N:] == 7.0).all()) and torch.equal(got, run(*case, group, dtype))
 
 
+@pytest.mark.parametrize("kernel,M,N,K", [(10, 3, 131077, 65664), (3, 40, 131077, 65664), (1, 70001, 32003, 130), (8, 70001, 35, 61500)])
+def test_arrays_beyond_32_bits(kernel, M, N, K, forced):
+    """More than 2^32 bytes of weights, of outputs or of codes: the first and last rows and channels are what the same kernel makes of them alone, bit by bit."""
+    tiles = -(-K // 128)
+    x = torch.randint(-127, 128, (tiles, M, 128), dtype=torch.int8, device="cuda")
+    w = torch.randint(0, 256, (tiles, N, 64), dtype=torch.uint8, device="cuda")
+    s, ws = torch.rand((M,), device="cuda"), torch.rand((tiles, N), device="cuda")
+    forced(kernel)
+    y = fptq.fptq_w4a8_linear(x, s, w, M, N, K, 128, ws)
+    assert max(x.numel(), w.numel(), 2 * y.numel()) > 2 ** 32
+    for rows in (slice(0, min(M, 300)), slice(max(M - 300, 0), M)):
+        for channels in (slice(0, min(N, 600)), slice(max(N - 600, 0), N)):
+            xs, wss, scales = x[:, rows].contiguous(), w[:, channels].contiguous(), ws[:, channels].contiguous()
+            part = fptq.fptq_w4a8_linear(xs, s[rows].clone(), wss, xs.shape[1], wss.shape[1], K, 128, scales)
+            assert torch.equal(y[rows, channels], part)
+
+
 def test_the_same_call_gives_the_same_bits():
     for M, N, K, group in ((1, 500, 4096, 128), (48, 300, 3000, 32), (400, 500, 2000, 64)):
         case = draw(M, N, K, group)

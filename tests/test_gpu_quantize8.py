@@ -168,6 +168,27 @@ def test_any_alignment_and_any_distance_between_rows(K, shift):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_arrays_beyond_32_bits():
+    """More than 2^32 bytes of inputs and 2^31 of codes."""
+    M, K = 600001, 4096
+    x = torch.randint(-(1 << 15), 1 << 15, (M, K), dtype=torch.int16, device="cuda").bitwise_and_(~0x4000).view(torch.bfloat16)      # magnitudes below 2
+    at = torch.tensor([0, 1, 262143, 262144, 524288, M - 2, M - 1])
+    picked = host(x[at.cuda()])
+    codes, scale, z = fptq.fptq_norm_quantize8(x, x, eps=1e-5)
+    _, u, inv = grouped.residual_norm(picked, picked, None, 1e-5)
+    want, want_scale = grouped.quantize_rows(u, inv)
+    assert np.array_equal(codes.view(-1, M, 128)[:, at.cuda()].cpu().numpy().reshape(-1), grouped.lay_out(want))
+    same_scales(scale[at.cuda()], want_scale)
+    assert np.array_equal(host(z[at.cuda()]), 2 * picked)
+    del z
+    codes, scale = fptq.fptq_gated_quantize8(x, x)
+    want, want_scale = grouped.quantize_rows(grouped.gated(picked, picked))
+    assert np.array_equal(codes.view(-1, M, 128)[:, at.cuda()].cpu().numpy().reshape(-1), grouped.lay_out(want))
+    assert np.array_equal(scale[at.cuda()].cpu().numpy(), want_scale)
+    del x, codes
+    torch.cuda.empty_cache()
+
+
 def test_more_rows_than_one_launch_takes():
     """A launch has 2^20 workgroups at most; they go on from row to row."""
     for M, K in ((4 * (1 << 20) + 5, 8), ((1 << 20) + 3, 1026)):
