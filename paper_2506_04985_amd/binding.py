@@ -629,7 +629,7 @@ def fptq_w4a8_linear(xq8, token_scale, wq, M, N, K, group, w_scales, out=None, o
     _dev(token_scale, torch.float32, "token_scale")
     _dev(wq, torch.uint8, "wq")
     _dev(w_scales, torch.float32, "w_scales")
-    if group < 1:
+    if not 1 <= group < 1 << 63:      # as many bits as the library takes: fewer scales would be asked for than it reads
         raise FptqError(-2, f"group must be 32, 64 or a multiple of 128 (got {group})")
     if xq8.numel() < _need8(M, K) or token_scale.numel() < M or wq.numel() < _need(N, K):
         raise FptqError(-3, "codes, token_scale or packed weights smaller than the shape needs")

@@ -661,7 +661,7 @@ hipError_t launch_grouped_linear(const uint8_t *x, const float *token_scale, con
 {
     const int64_t kt = k_tiles(K), per = group > KT ? (group / KT < kt ? group / KT : kt) : 1;
     const Choice choice = chosen(M, N, K, group, scratch ? (scratch_bytes < MOST_SCRATCH ? scratch_bytes : MOST_SCRATCH) : 0);
-    const GroupedCall c = {x, token_scale, w, (int)M, (int)N, (int)kt, (int)((K + group - 1) / group), (uint32_t)per, scales, y, y_type, s, choice.splits, (float *)scratch};
+    const GroupedCall c = {x, token_scale, w, (int)M, (int)N, (int)kt, (int)((K - 1) / group + 1), (uint32_t)per, scales, y, y_type, s, choice.splits, (float *)scratch};
     return group == 32 ? launch_choice<4>(choice.kernel, c) : group == 64 ? launch_choice<2>(choice.kernel, c) : launch_choice<1>(choice.kernel, c);
 }
 

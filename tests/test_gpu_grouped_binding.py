@@ -49,6 +49,7 @@ def test_what_is_refused(both):  # noqa: F811
                      (lambda: gated(x, r[:-1]), fptq.FptqError), (lambda: gated(x, r.float()), TypeError), (lambda: gated(x.t(), r.t()), TypeError), (lambda: gated(x[0], r[0]), TypeError),
                      (lambda: gated(x, x[:1].expand(M, K)), fptq.FptqError),
                      (lambda: lin(codes, scale, w, M, N, K, 48, ws), fptq.FptqError), (lambda: lin(codes, scale, w, M, N, K, 0, ws), fptq.FptqError),
+                     (lambda: lin(codes, scale, w, M, N, K, (1 << 64) + 128, ws), fptq.FptqError),
                      (lambda: lin(codes, scale, w, M, N, K, 32, ws), fptq.FptqError), (lambda: lin(codes, scale, w, M + 1, N, K, 64, ws), fptq.FptqError),
                      (lambda: lin(codes, scale, w, M, N + 1, K, 64, ws), fptq.FptqError), (lambda: lin(codes, scale[:-1], w, M, N, K, 64, ws), fptq.FptqError),
                      (lambda: lin(codes.view(torch.uint8), scale, w, M, N, K, 64, ws), TypeError), (lambda: lin(codes, scale.double(), w, M, N, K, 64, ws), TypeError),

@@ -108,7 +108,7 @@ def test_one_scale_a_channel(M):
     N, K = 96, 700
     case = draw(M, N, K, 768)
     y, mass = grouped.linear(*case[:3], 768, case[3])
-    for group in (768, 1 << 20):
+    for group in (768, 1 << 20, (1 << 63) - 128):
         check(run(*case, group), y, mass, K, 768)
 
 
