@@ -171,8 +171,8 @@ __device__ inline void store_four(v4f v, float scale, int t, int n, int N, void 
 // nobody waits for another before the end.
 //
 // What bounds the large tiles: those conversions beside the MFMAs, then power.  An MFMA takes 33.5 cycles alone, with four conversions and four multiply-adds behind it 51 (two waves a SIMD,
-// measured in registers); 256 x 256 walks a K tile in 1.50 us on zeros, 56 cycles an MFMA, and in 1.9 on dense operands, where the clock falls to 1.75 GHz (4096 x 28672 x 4096 485 to 515 us, 1.9 to
-// 2.0 POP/s; MFMAs busy in 45 % of the cycles).  Two waves a SIMD, so that one's conversions run under the other's MFMAs; within a wave they are pinned behind the MFMAs of the next
+// measured in registers); 256 x 256 walks a K tile in 1.50 us on zeros, 56 cycles an MFMA, and in 1.9 on dense operands, where the clock falls to 1.75 GHz (4096 x 28672 x 4096 478 to 511 us, 1.9 to
+// 2.0 POP/s; MFMAs busy in 47 % of the cycles).  Two waves a SIMD, so that one's conversions run under the other's MFMAs; within a wave they are pinned behind the MFMAs of the next
 // unit, without which that launch took 539 us on a card where it now takes 514.
 typedef int v16i __attribute__((ext_vector_type(16)));
 

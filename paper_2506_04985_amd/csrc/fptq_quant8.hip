@@ -7,7 +7,7 @@
 // The norm's factor is the same for a whole row, so it goes into the token's scale and not into the codes: one pass with one exchange between
 // the waves of a row (a sum and a maximum at once), and a row's codes do not wait for a division and a root in 64 bits.  The row stays in registers
 // from its load to its codes.  Bound: HBM, 2 to 4 bytes read and 1 to 3 written per value: norm with residual and gain 8192 x 8192 83 us, 5.65 TB/s (a copy of 2 GiB reaches 4.92), VALU busy in
-// 40 % of the cycles; gated 4096 x 14336 58 us, 5.06 TB/s.  Few rows are a chain of latencies: launch, row, exchange, store (norm 1 x 4096 2.2 us in a kernel trace, gated 16 x 14336 5.4).
+// 40 % of the cycles; gated 4096 x 14336 58 us, 5.06 TB/s.  Few rows are a chain of latencies: launch, row, exchange, store (norm 1 x 4096 2.2 us in a kernel trace, gated 16 x 14336 5.4 to 5.8).
 #include "fptq_common.h"
 
 namespace fptq {
