@@ -174,6 +174,10 @@ __device__ inline void store_four(v4f v, float scale, int t, int n, int N, void 
 // measured in registers); 256 x 256 walks a K tile in 1.50 us on zeros, 56 cycles an MFMA, and in 1.9 on dense operands, where the clock falls to 1.75 GHz (4096 x 28672 x 4096 478 to 511 us, 1.9 to
 // 2.0 POP/s; MFMAs busy in 47 % of the cycles).  Two waves a SIMD, so that one's conversions run under the other's MFMAs; within a wave they are pinned behind the MFMAs of the next
 // unit, without which that launch took 539 us on a card where it now takes 514.
+//
+// The MFMAs start from 0x4b400000, the pattern of the float 1.5 * 2^23: a sum below 2^22 (128 terms of at most 127 * 128 come to 2^21) is added to its low bits, and the result, taken as a float, less
+// 1.5 * 2^23 is the sum exactly.  The subtraction issues at twice the conversion's rate: 2048 x 28672 x 4096 with groups of 32 491 us with conversions, 475 so; 1000 x 4096 x 14336 on 256 x 192 with
+// groups of 64 199 and 191; 4096 x 28672 x 4096 504 and 496.
 typedef int v16i __attribute__((ext_vector_type(16)));
 
 template <int WAVES_N_, int WAVES_M_, int TN_, int TM_, int STAGES_, int KS_, int GT_>
@@ -183,7 +187,8 @@ struct Tile {
     static constexpr int X_BYTES = BM * KT, W_BYTES = BN * SEG, S_BYTES = BN * GT * 4, STAGE_BYTES = X_BYTES + W_BYTES + S_BYTES;
     static constexpr int X_LOADS = X_BYTES / (WAVES * 1024), W_LOADS = W_BYTES / (WAVES * 1024), S_PIECES = BN * GT / 64, S_LOADS = (S_PIECES + WAVES - 1) / WAVES;
     static constexpr int LOADS = X_LOADS + W_LOADS + S_LOADS, RING_BYTES = STAGES * STAGE_BYTES;
-    static constexpr int SETS = TN * TM * 16 <= 96 && TM > 1 ? 2 : 1;
+    static constexpr int SETS = TN * TM * 16 <= 96 && TM > 1 && TN * TM * GT < 24 ? 2 : 1;
+    static constexpr bool PRESET = TN * TM < 8 || GT == 1;      // where the constants' 16 registers do not spill
     static constexpr int OUT_ROWS = WAVES_M * 32, OUT_BYTES = KS * OUT_ROWS * BN * 4;      // a pass of the epilogue
     static constexpr int PASSES = TM > 1 && 2 * OUT_BYTES <= KS * RING_BYTES ? 2 : 1;      // of them that LDS holds
     static constexpr int SCALES_AT = KS * RING_BYTES > OUT_BYTES ? KS * RING_BYTES : OUT_BYTES, LDS_BYTES = SCALES_AT + BM * 4;      // the tokens' scales lie behind
@@ -274,7 +279,13 @@ __global__ __launch_bounds__(C::THREADS, 2) void grouped_tile_kernel(const uint8
     // where there is room, into others and a unit earlier, and loads of a later K tile are issued.
     constexpr int MFMAS = 4 / C::GT, UNITS = C::TN * C::TM * C::GT, LAST = UNITS - 1, FIRST = UNITS > 2 ? 1 : 0, PER_UNIT = (C::LOADS + LAST - FIRST - 1) / (LAST - FIRST);
     static_assert(UNITS % 2 == 0, "units take two sets of accumulators in turn");
-    v16i acc[2] = {};
+    v16i none = {};
+    if (C::PRESET) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) none[r] = 0x4b400000;
+        asm volatile("" : "+v"(none));      // kept in registers: as constants they would be moved there for every unit
+    }
+    v16i acc[2] = {none, none};
     v4i xo[C::SETS][4], wo[C::TN][4], raw[C::TN][2];
     float sc[C::TN][C::GT], sc_last = 0.0f;
     const int steps = (kt1 - kt0 + C::KS - 1) / C::KS;      // the same for all sets: they share the barriers
@@ -325,7 +336,7 @@ __global__ __launch_bounds__(C::THREADS, 2) void grouped_tile_kernel(const uint8
     };
     auto convert = [&](const v16i &a, float s, float (&f)[16]) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) f[r] = __builtin_fmaf((float)a[r], s, f[r]);
+        for (int r = 0; r < 16; ++r) f[r] = __builtin_fmaf(C::PRESET ? __uint_as_float((uint32_t)a[r]) - 12582912.0f : (float)a[r], s, f[r]);
     };
     int stage = 0;
     for (int step = 0; step < steps; ++step) {
@@ -346,7 +357,7 @@ __global__ __launch_bounds__(C::THREADS, 2) void grouped_tile_kernel(const uint8
             constexpr bool reads = tn == (C::SETS == 1 ? C::TN - 1 : 0) && tm + 1 < C::TM, widening = tm == 0 && g == 0 && tn + 1 < C::TN;
             constexpr int at = (u - FIRST) * PER_UNIT, loads = u < FIRST || at >= C::LOADS ? 0 : C::LOADS - at < PER_UNIT ? C::LOADS - at : PER_UNIT;
             constexpr int valu = (32 + (widening ? 24 : 0) + MFMAS - 1) / MFMAS;
-            v16i a = {};
+            v16i a = none;
 #pragma unroll
             for (int m = 0; m < MFMAS; ++m) a = __builtin_amdgcn_mfma_i32_32x32x32_i8(xo[tm % C::SETS][g * MFMAS + m], wo[tn][g * MFMAS + m], a, 0, 0, 0);
             convert(acc[p % 2], u == 0 ? sc_last : sc[p / C::GT % C::TN][p % C::GT], sum[p / C::GT % C::TN][p / (C::TN * C::GT)]);
@@ -424,8 +435,8 @@ __global__ __launch_bounds__(256) void grouped_join_kernel(const float *__restri
 //
 // What a tile shape's launch takes, in us, fitted on 5636 problems of random sizes (17 to 6000 tokens, 256 to 60000 channels, K up to 16384, weights not in any cache; 2464 of them in
 // groups of 128, 1552 in groups of 64, 1620 in groups of 32), each run with every shape on an MI355X: `start`, and for every CU, `fit` workgroups at a time, `fixed` and `step` a K tile of
-// a set, which depend on how many run there together.  Against the best of these eight and of four few-token kernels the choice takes, from 65 tokens on, 0.3 to 0.7 % longer on average
-// and 2 to 5 % at the 95th percentile, and up to 64 tokens 1.4 to 1.9 and 8 to 9 %.
+// a set, which depend on how many run there together.  On 6073 others, against the best of these eight and of four few-token kernels, the choice takes, from 65 tokens on, 0.3 to 0.8 % longer
+// on average and 2 to 6 % at the 95th percentile, and up to 64 tokens 1.6 to 1.7 and 9 to 11 %.
 struct TileCost {
     int bn, bm, sets, fit;
     float start, fixed[3], step[3];
