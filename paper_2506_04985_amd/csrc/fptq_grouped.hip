@@ -170,9 +170,9 @@ __device__ inline void store_four(v4f v, float scale, int t, int n, int N, void 
 // vector instructions that the 4 MFMAs of a 128-value group cost.  KS sets of WAVES waves share the tile, set g taking K tiles g, g + KS, ... through a ring of its own; with one wave in a set
 // nobody waits for another before the end.
 //
-// What bounds the large tiles: those conversions beside the MFMAs, then power.  An MFMA takes 33.5 cycles alone, with four conversions and four multiply-adds behind it 51 (two waves a SIMD,
-// measured in registers); 256 x 256 walks a K tile in 1.50 us on zeros, 56 cycles an MFMA, and in 1.9 on dense operands, where the clock falls to 1.75 GHz (4096 x 28672 x 4096 478 to 511 us, 1.9 to
-// 2.0 POP/s; MFMAs busy in 47 % of the cycles).  Two waves a SIMD, so that one's conversions run under the other's MFMAs; within a wave they are pinned behind the MFMAs of the next
+// What bounds the large tiles: those conversions beside the MFMAs, then power.  An MFMA takes 33.5 cycles alone, with four conversions and four multiply-adds behind it 51, with eight multiply-adds 47.6 (two waves a
+// SIMD, measured in registers); 256 x 256 walks a K tile in 1.50 us on zeros, 56 cycles an MFMA, and in 1.9 on dense operands, where the clock falls to 1.75 GHz (4096 x 28672 x 4096 464 to 497 us, 1.9 to
+// 2.1 POP/s; MFMAs busy in 47 % of the cycles).  Two waves a SIMD, so that one's conversions run under the other's MFMAs; within a wave they are pinned behind the MFMAs of the next
 // unit, without which that launch took 539 us on a card where it now takes 514.
 //
 // The MFMAs start from 0x4b400000, the pattern of the float 1.5 * 2^23: a sum below 2^22 (128 terms of at most 127 * 128 come to 2^21) is added to its low bits, and the result, taken as a float, less
