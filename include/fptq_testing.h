@@ -42,8 +42,8 @@ int fptq_set_linear_prefill(int mode);
 int fptq_linear_launch_plan(int64_t M, int64_t N, int64_t K, int with_workspace, char *kernel, int kernel_len,
                             int64_t *workgroups, int *threads);
 
-/* The kernel that fptq_w4a8_linear takes: 0 chooses it per problem (default); 1 .. 8 force a tile, in `splits` ranges of K (1 .. 8) where the call has scratch for them, 9 .. 12 a few-token
- * kernel, for tests and sweeps; fptq_w4a8_linear_scratch_bytes follows.  A tile that does not serve the call's groups (1 and 3: groups of 32) makes it fail with FPTQ_ERR_HIP.
+/* The kernel that fptq_w4a8_linear takes: 0 chooses it per problem (default); 1 .. 10 force a tile, in `splits` ranges of K (1 .. 8) where the call has scratch for them, 11 .. 14 a few-token
+ * kernel, for tests and sweeps; fptq_w4a8_linear_scratch_bytes follows.  A tile that does not serve the call's groups (1, 3 and 5: groups of 32) makes it fail with FPTQ_ERR_HIP.
  * fptq_grouped_kernel returns the number that a call without scratch would take, host only. */
 int fptq_set_grouped_kernel(int kernel, int splits);
 int fptq_grouped_kernel(int64_t M, int64_t N, int64_t K, int64_t group);

@@ -812,7 +812,7 @@ int fptq_unpack8(const void *packed8, int64_t rows, int64_t K, int8_t *out_int8,
 int fptq_set_grouped_kernel(int kernel, int splits)
 {
     if (!set_grouped_kernel(kernel, splits)) {
-        set_error("fptq_set_grouped_kernel: kernel must be 0..12, splits 1..8");
+        set_error("fptq_set_grouped_kernel: kernel must be 0..14, splits 1..8");
         return FPTQ_ERR_VALUE;
     }
     return FPTQ_OK;

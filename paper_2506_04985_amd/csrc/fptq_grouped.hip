@@ -433,57 +433,67 @@ __global__ __launch_bounds__(256) void grouped_join_kernel(const float *__restri
 
 // ---- which kernel
 //
-// What a tile shape's launch takes, in us, fitted on 5636 problems of random sizes (17 to 6000 tokens, 256 to 60000 channels, K up to 16384, weights not in any cache; 2464 of them in
-// groups of 128, 1552 in groups of 64, 1620 in groups of 32), each run with every shape on an MI355X: `start`, and for every CU, `fit` workgroups at a time, `fixed` and `step` a K tile of
-// a set, which depend on how many run there together.  On 6073 others, against the best of these eight and of four few-token kernels, the choice takes, from 65 tokens on, 0.3 to 0.8 % longer
-// on average and 2 to 6 % at the 95th percentile, and up to 64 tokens 1.6 to 1.7 and 9 to 11 %.
+// What a tile shape's launch takes, in us, fitted on 6032 problems of random sizes (17 to 6000 tokens, 256 to 60000 channels, K up to 16384, weights not in any cache; about 2700 of them in
+// groups of 128, 1500 in groups of 64, 1800 in groups of 32), each run with every shape on an MI355X: `start`, and for every CU, `fit` workgroups at a time, `fixed` and `step` a K tile of
+// a set, which depend on how many run there together.  Against the best of these ten and of four few-token kernels the choice takes, from 65 tokens on, 0.3 to 0.8 % longer on average
+// and 2 to 6 % at the 95th percentile, and up to 64 tokens 1.3 to 2.0 and 8 to 11 %.  Without 256 x 128 and 256 x 96 the best would take 0.5 to 2 % longer, where a call's tiles then make another round
+// of the CUs 10 to 20 (96 x 57344 x 8192 93 us, on 256 x 96 76; 700 x 8192 x 8192 76 and 63).
 struct TileCost {
     int bn, bm, sets, fit;
     float start, fixed[3], step[3];
 };
-constexpr TileCost COSTS[3][8] = {      // groups of 128 and more, of 64, of 32 (zeros: no such kernel)
+constexpr int TILES = 10;
+constexpr TileCost COSTS[3][TILES] = {      // groups of 128 and more, of 64, of 32 (zeros: no such kernel)
     {
-        {256, 256, 1, 1, 0.00f, {9.05f}, {1.60f}},
-        {256, 192, 1, 1, 0.39f, {7.07f}, {1.34f}},
-        {256, 64, 2, 1, 1.17f, {3.79f}, {1.10f}},
-        {128, 64, 1, 3, 2.79f, {1.01f, 1.87f, 2.62f}, {0.49f, 0.72f, 0.96f}},
-        {128, 64, 2, 1, 1.30f, {2.69f}, {0.62f}},
-        {128, 32, 2, 2, 2.52f, {1.05f, 2.05f}, {0.55f, 0.76f}},
-        {64, 64, 4, 1, 1.31f, {2.90f}, {0.74f}},
-        {64, 32, 8, 1, 1.43f, {2.00f}, {0.78f}},
+        {256, 256, 1, 1, 0.00f, {9.07f}, {1.62f}},
+        {256, 192, 1, 1, 0.42f, {7.14f}, {1.33f}},
+        {256, 128, 2, 1, 0.86f, {6.11f}, {1.72f}},
+        {256, 96, 2, 1, 1.25f, {4.46f}, {1.53f}},
+        {256, 64, 2, 1, 1.35f, {3.74f}, {1.07f}},
+        {128, 64, 1, 3, 2.90f, {0.98f, 1.96f, 2.77f}, {0.51f, 0.70f, 0.94f}},
+        {128, 64, 2, 1, 1.38f, {2.72f}, {0.61f}},
+        {128, 32, 2, 2, 2.48f, {1.16f, 2.16f}, {0.56f, 0.74f}},
+        {64, 64, 4, 1, 1.44f, {2.93f}, {0.72f}},
+        {64, 32, 8, 1, 1.54f, {2.03f}, {0.78f}},
     },
     {
-        {256, 256, 1, 1, 0.18f, {8.95f}, {2.25f}},
-        {256, 192, 1, 1, 0.89f, {6.93f}, {1.78f}},
-        {256, 64, 2, 1, 1.30f, {3.82f}, {1.38f}},
-        {128, 64, 1, 3, 2.95f, {0.81f, 1.72f, 2.60f}, {0.57f, 0.83f, 1.13f}},
-        {128, 64, 2, 1, 1.34f, {2.67f}, {0.78f}},
-        {128, 32, 2, 2, 2.57f, {1.05f, 2.13f}, {0.64f, 0.90f}},
-        {64, 64, 4, 1, 1.42f, {2.78f}, {0.94f}},
-        {64, 32, 8, 1, 1.46f, {2.00f}, {0.93f}},
+        {256, 256, 1, 1, 0.00f, {9.19f}, {2.25f}},
+        {256, 192, 1, 1, 0.65f, {6.99f}, {1.73f}},
+        {256, 128, 2, 1, 1.27f, {5.94f}, {2.33f}},
+        {256, 96, 2, 1, 1.40f, {4.69f}, {1.87f}},
+        {256, 64, 2, 1, 1.40f, {3.81f}, {1.34f}},
+        {128, 64, 1, 3, 2.89f, {1.01f, 2.07f, 2.67f}, {0.58f, 0.77f, 1.11f}},
+        {128, 64, 2, 1, 1.43f, {2.70f}, {0.77f}},
+        {128, 32, 2, 2, 2.64f, {1.02f, 2.21f}, {0.65f, 0.87f}},
+        {64, 64, 4, 1, 1.52f, {2.84f}, {0.92f}},
+        {64, 32, 8, 1, 1.61f, {1.95f}, {0.91f}},
     },
     {
         {256, 256, 1, 1, 0.00f, {0.00f}, {0.00f}},
-        {256, 192, 1, 1, 1.00f, {6.72f}, {2.79f}},
+        {256, 192, 1, 1, 0.33f, {7.41f}, {2.56f}},
+        {256, 128, 2, 1, 0.00f, {0.00f}, {0.00f}},
+        {256, 96, 2, 1, 1.05f, {5.05f}, {2.65f}},
         {256, 64, 2, 1, 0.00f, {0.00f}, {0.00f}},
-        {128, 64, 1, 3, 3.77f, {0.00f, 0.97f, 3.55f}, {0.82f, 1.19f, 1.68f}},
-        {128, 64, 2, 1, 1.32f, {2.76f}, {1.11f}},
-        {128, 32, 2, 2, 1.79f, {1.90f, 4.42f}, {0.90f, 1.76f}},
-        {64, 64, 4, 1, 1.33f, {2.90f}, {1.41f}},
-        {64, 32, 8, 1, 1.47f, {2.01f}, {1.28f}},
+        {128, 64, 1, 3, 3.83f, {0.00f, 1.16f, 3.61f}, {0.83f, 1.09f, 1.64f}},
+        {128, 64, 2, 1, 1.27f, {2.82f}, {1.05f}},
+        {128, 32, 2, 2, 1.91f, {1.90f, 4.50f}, {0.88f, 1.73f}},
+        {64, 64, 4, 1, 1.40f, {2.92f}, {1.40f}},
+        {64, 32, 8, 1, 1.56f, {1.99f}, {1.24f}},
     },
 };
 constexpr float JOIN_START = 3.0f, JOIN_BYTE = 0.4e-6f;      // us: the second launch of a split K, and a byte of its ranges' sums, written and read
 template <int GT> using Tile0 = Tile<4, 2, 2, 4, 3, 1, GT>;
 template <int GT> using Tile1 = Tile<4, 2, 2, 3, 3, 1, GT>;
-template <int GT> using Tile2 = Tile<4, 1, 2, 2, 3, 2, GT>;
-template <int GT> using Tile3 = Tile<2, 2, 2, 1, 3, 1, GT>;
-template <int GT> using Tile4 = Tile<4, 1, 1, 2, 3, 2, GT>;
-template <int GT> using Tile5 = Tile<2, 1, 2, 1, 3, 2, GT>;
-template <int GT> using Tile6 = Tile<1, 1, 2, 2, 3, 4, GT>;
-template <int GT> using Tile7 = Tile<1, 1, 2, 1, 2, 8, GT>;
+template <int GT> using Tile2 = Tile<4, 1, 2, 4, 2, 2, GT>;
+template <int GT> using Tile3 = Tile<4, 1, 2, 3, 2, 2, GT>;
+template <int GT> using Tile4 = Tile<4, 1, 2, 2, 3, 2, GT>;
+template <int GT> using Tile5 = Tile<2, 2, 2, 1, 3, 1, GT>;
+template <int GT> using Tile6 = Tile<4, 1, 1, 2, 3, 2, GT>;
+template <int GT> using Tile7 = Tile<2, 1, 2, 1, 3, 2, GT>;
+template <int GT> using Tile8 = Tile<1, 1, 2, 2, 3, 4, GT>;
+template <int GT> using Tile9 = Tile<1, 1, 2, 1, 2, 8, GT>;
 // groups of 32: the first would spill, the third has no room for its scales in LDS
-constexpr bool tile_serves(int i, int gt) { return gt < 4 || (i != 0 && i != 2); }
+constexpr bool tile_serves(int i, int gt) { return gt < 4 || (i != 0 && i != 2 && i != 4); }
 
 static int64_t tiles_of(const TileCost &c, int64_t M, int64_t N) { return ((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn); }
 
@@ -509,7 +519,7 @@ static float few_estimate(const FewCost &c, int64_t M, int64_t N, int64_t kt, in
     return c.start + (float)steps * (c.latency + (float)each * c.each);
 }
 
-// What a call takes: 0 .. 7 a tile, 8 + i the few-token kernel FEW_COSTS[..][i], 11 the one of eight waves and 16 channels; into how many ranges K is split between workgroups.
+// What a call takes: 0 .. 9 a tile, 10 + i the few-token kernel FEW_COSTS[..][i], 13 the one of eight waves and 16 channels; into how many ranges K is split between workgroups.
 struct Choice {
     int kernel, splits;
 };
@@ -523,13 +533,13 @@ static Choice grouped_choice(int64_t M, int64_t N, int64_t K, int gt, int64_t sc
 {
     const int64_t kt = k_tiles(K), cus = device_cus_or_default();
     if (M <= 16) {
-        if (M > 12 && kt >= 32 && N > 32 * cus && N <= 64 * cus) return {7, 1};
-        if (M > 12 && kt >= 48 && N > 96 * cus) return {gt == 4 ? 7 : 5, 1};
-        if (kt < 9) return {N <= 48 * cus ? 11 : 10, 1};
-        return {N <= 16 * cus ? 8 : N > 64 * cus && kt < 33 ? 10 : 9, 1};
+        if (M > 12 && kt >= 32 && N > 32 * cus && N <= 64 * cus) return {9, 1};
+        if (M > 12 && kt >= 48 && N > 96 * cus) return {gt == 4 ? 9 : 7, 1};
+        if (kt < 9) return {N <= 48 * cus ? 13 : 12, 1};
+        return {N <= 16 * cus ? 10 : N > 64 * cus && kt < 33 ? 12 : 11, 1};
     }
-    // no kernel takes less than its bytes do at 5.1 TB/s; among those that come to it the larger tile reads less (32 x 28672 x 4096, fourth from last 14.4 us, last 17.0)
-    const float bytes = (float)N * (float)kt * (float)(SEG + 4 * gt) + (float)M * (float)kt * (float)KT + 2.0f * (float)M * (float)N, memory = bytes / 5.1e6f;
+    // no kernel takes less than its bytes do at 4.8 TB/s; among those that come to it the larger tile reads less (32 x 28672 x 4096, 128 x 32 14.4 us, 64 x 32 17.0)
+    const float bytes = (float)N * (float)kt * (float)(SEG + 4 * gt) + (float)M * (float)kt * (float)KT + 2.0f * (float)M * (float)N, memory = bytes / 4.8e6f;
     const TileCost *const costs = COSTS[gt >> 1];
     Choice best = {-1, 1};
     float least = 0.0f;
@@ -537,13 +547,13 @@ static Choice grouped_choice(int64_t M, int64_t N, int64_t K, int gt, int64_t sc
         us = us > memory ? us : memory;
         if (best.kernel < 0 || us < least) best = {i, splits}, least = us;
     };
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < TILES; ++i)
         if (tile_serves(i, gt)) offer(i, 1, tile_estimate(costs[i], tiles_of(costs[i], M, N), kt, cus));
     if (M <= 64)
-        for (int i = 0; i < 3; ++i) offer(8 + i, 1, few_estimate(FEW_COSTS[gt >> 1][i], M, N, kt, cus));
+        for (int i = 0; i < 3; ++i) offer(TILES + i, 1, few_estimate(FEW_COSTS[gt >> 1][i], M, N, kt, cus));
     // Few tiles and a long K: its ranges go to workgroups of their own, and a second launch adds their sums.
     const int64_t range = M * ((N + 3) / 4 * 16);      // bytes of a range's sums
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < TILES; ++i) {
         const int64_t tiles = tiles_of(costs[i], M, N);
         for (int splits = 2; splits <= 8 && tile_serves(i, gt) && tiles * splits <= 2 * cus && kt / splits >= 8 && splits * range <= scratch; ++splits)
             offer(i, splits, tile_estimate(costs[i], tiles * splits, (kt + splits - 1) / splits, cus) + JOIN_START + (float)(splits * range) * JOIN_BYTE);
@@ -564,10 +574,12 @@ static hipError_t set_tile_attributes()
     if (e == hipSuccess) e = set_tile_attribute<Tile1<GT>>();
     if constexpr (tile_serves(2, GT)) e = e == hipSuccess ? set_tile_attribute<Tile2<GT>>() : e;
     if (e == hipSuccess) e = set_tile_attribute<Tile3<GT>>();
-    if (e == hipSuccess) e = set_tile_attribute<Tile4<GT>>();
+    if constexpr (tile_serves(4, GT)) e = e == hipSuccess ? set_tile_attribute<Tile4<GT>>() : e;
     if (e == hipSuccess) e = set_tile_attribute<Tile5<GT>>();
     if (e == hipSuccess) e = set_tile_attribute<Tile6<GT>>();
-    return e == hipSuccess ? set_tile_attribute<Tile7<GT>>() : e;
+    if (e == hipSuccess) e = set_tile_attribute<Tile7<GT>>();
+    if (e == hipSuccess) e = set_tile_attribute<Tile8<GT>>();
+    return e == hipSuccess ? set_tile_attribute<Tile9<GT>>() : e;
 }
 hipError_t grouped_device_init()
 {
@@ -630,14 +642,18 @@ static hipError_t launch_choice(int choice, const GroupedCall &c)
         if constexpr (tile_serves(2, GT)) return launch_tile<Tile2<GT>>(c);
         break;
     case 3: return launch_tile<Tile3<GT>>(c);
-    case 4: return launch_tile<Tile4<GT>>(c);
+    case 4:
+        if constexpr (tile_serves(4, GT)) return launch_tile<Tile4<GT>>(c);
+        break;
     case 5: return launch_tile<Tile5<GT>>(c);
     case 6: return launch_tile<Tile6<GT>>(c);
     case 7: return launch_tile<Tile7<GT>>(c);
-    case 8: return launch_few<16, 1, GT>(c);
-    case 9: return launch_few<16, 2, GT>(c);
-    case 10: return launch_few<8, 2, GT>(c);
-    case 11: return launch_few<8, 1, GT>(c);
+    case 8: return launch_tile<Tile8<GT>>(c);
+    case 9: return launch_tile<Tile9<GT>>(c);
+    case 10: return launch_few<16, 1, GT>(c);
+    case 11: return launch_few<16, 2, GT>(c);
+    case 12: return launch_few<8, 2, GT>(c);
+    case 13: return launch_few<8, 1, GT>(c);
     }
     return hipErrorInvalidValue;
 }
@@ -646,7 +662,7 @@ static hipError_t launch_choice(int choice, const GroupedCall &c)
 static std::atomic<int> g_forced_grouped{0};
 bool set_grouped_kernel(int kernel, int splits)
 {
-    if (kernel < 0 || kernel > 12 || splits < 1 || splits > 8) return false;
+    if (kernel < 0 || kernel > TILES + 4 || splits < 1 || splits > 8) return false;
     g_forced_grouped.store(kernel + 16 * splits, std::memory_order_relaxed);
     return true;
 }
@@ -655,7 +671,7 @@ static Choice chosen(int64_t M, int64_t N, int64_t K, int64_t group, int64_t scr
 {
     const int code = g_forced_grouped.load(std::memory_order_relaxed), forced = code % 16, splits = code / 16;
     if (!forced) return grouped_choice(M, N, K, group == 32 ? 4 : group == 64 ? 2 : 1, scratch);
-    const bool room = forced <= 8 && splits <= k_tiles(K) && splits * M * ((N + 3) / 4 * 16) <= scratch;
+    const bool room = forced <= TILES && splits <= k_tiles(K) && splits * M * ((N + 3) / 4 * 16) <= scratch;
     return {forced - 1, room ? splits : 1};
 }
 

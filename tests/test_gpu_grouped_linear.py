@@ -70,14 +70,14 @@ def forced():
 
 
 @pytest.mark.parametrize("group", [32, 64, 128, 256])
-@pytest.mark.parametrize("kernel", range(1, 13))
+@pytest.mark.parametrize("kernel", range(1, 15))
 def test_every_kernel(kernel, group, forced):
     """Each kernel on sizes that cut its tiles, sets of K tiles and groups; a single K tile, fewer than it has sets, and many."""
     for M, N, K in ((1, 1, 1), (70, 90, 100), (33, 257, 640), (300, 520, 1100), (257, 129, 2600), (5, 64, 129)):
         case = draw(M, N, K, group, kernel)
         y, mass = grouped.linear(*case[:3], group, case[3])
         forced(kernel)
-        if group == 32 and kernel in (1, 3):
+        if group == 32 and kernel in (1, 3, 5):
             with pytest.raises(fptq.FptqError):
                 run(*case, group)
             continue
@@ -86,7 +86,7 @@ def test_every_kernel(kernel, group, forced):
 
 
 @pytest.mark.parametrize("splits", [2, 3, 8])
-@pytest.mark.parametrize("kernel,group", [(k, g) for k in range(1, 9) for g in (32, 64, 128, 256) if g != 32 or k not in (1, 3)])
+@pytest.mark.parametrize("kernel,group", [(k, g) for k in range(1, 11) for g in (32, 64, 128, 256) if g != 32 or k not in (1, 3, 5)])
 def test_ranges_of_k(kernel, group, splits, forced):
     """K cut between workgroups: ranges of several K tiles, of one, and without any; a caller's scratch, more than needed and full of NaN."""
     for M, N, K in ((70, 90, 100), (33, 257, 1100), (257, 129, 2600)):
@@ -149,7 +149,7 @@ def test_nothing_is_written_behind_the_last_row(M, N, K, group, dtype):
     assert bool((whole[M * N:] == 7.0).all()) and torch.equal(got, run(*case, group, dtype))
 
 
-@pytest.mark.parametrize("kernel,M,N,K", [(10, 3, 131077, 65664), (3, 40, 131077, 65664), (1, 70001, 32003, 130), (8, 70001, 35, 61500)])
+@pytest.mark.parametrize("kernel,M,N,K", [(12, 3, 131077, 65664), (5, 40, 131077, 65664), (1, 70001, 32003, 130), (10, 70001, 35, 61500)])
 def test_arrays_beyond_32_bits(kernel, M, N, K, forced):
     """More than 2^32 bytes of weights, of outputs or of codes: the first and last rows and channels are what the same kernel makes of them alone, bit by bit."""
     tiles = -(-K // 128)

@@ -62,16 +62,17 @@ def test_sizes_and_unpack():
 def test_kernel_choice_is_host_arithmetic():
     """On 256 CUs: a few-token kernel up to 16 tokens by two lines, then the least of the fitted times."""
     L = fptq.lib()
-    for bad in ((-1, 1), (13, 1), (3, 0), (3, 9)):
+    for bad in ((-1, 1), (15, 1), (3, 0), (3, 9)):
         assert L.fptq_set_grouped_kernel(*bad) == VALUE
     assert L.fptq_w4a8_linear_scratch_bytes(0, 1, 1, 128) == SHAPE and L.fptq_w4a8_linear_scratch_bytes(64, 64, 64, 100) == SHAPE
     for M, N, K in ((1, 4096, 14336), (16, 4096, 14336), (64, 28672, 4096), (4096, 28672, 4096), (1000, 4096, 14336)):
         assert L.fptq_w4a8_linear_scratch_bytes(M, N, K, 128) == 0
     of = L.fptq_grouped_kernel
     assert of(0, 1, 1, 32) == SHAPE and of(1, 1, 1, 0) == SHAPE
-    assert of(1, 4096, 4096, 128) == 9 and of(1, 6144, 4096, 128) == 10 and of(8, 128256, 4096, 64) == 11 and of(12, 28672, 14336, 128) == 10 and of(16, 28672, 14336, 128) == 6 and of(16, 28672, 14336, 32) == 8 and of(3, 4096, 512, 128) == 12
-    assert of(4096, 28672, 4096, 128) == 1 and of(333, 32003, 2504, 64) == 2 and of(1000, 4096, 14336, 128) == 3 and of(32, 28672, 4096, 128) == 6
+    assert of(1, 4096, 4096, 128) == 11 and of(1, 6144, 4096, 128) == 12 and of(8, 128256, 4096, 64) == 13 and of(12, 28672, 14336, 128) == 12
+    assert of(16, 28672, 14336, 128) == 8 and of(16, 28672, 14336, 32) == 10 and of(3, 4096, 512, 128) == 14
+    assert of(4096, 28672, 4096, 128) == 1 and of(333, 32003, 2504, 64) == 2 and of(1000, 4096, 14336, 128) == 5 and of(32, 28672, 4096, 128) == 8
     for M in (17, 64, 65, 500, 3000):
         for N in (64, 1000, 5000, 40000):
             for K in (128, 1000, 8000):
-                assert of(M, N, K, 32) not in (1, 3) and 1 <= of(M, N, K, 128) <= (11 if M <= 64 else 8)
+                assert of(M, N, K, 32) not in (1, 3, 5) and 1 <= of(M, N, K, 128) <= (13 if M <= 64 else 10)
