@@ -192,6 +192,8 @@ struct Tile {
     static constexpr int OUT_ROWS = WAVES_M * 32, OUT_BYTES = KS * OUT_ROWS * BN * 4;      // a pass of the epilogue
     static constexpr int PASSES = TM > 1 && 2 * OUT_BYTES <= KS * RING_BYTES ? 2 : 1;      // of them that LDS holds
     static constexpr int SCALES_AT = KS * RING_BYTES > OUT_BYTES ? KS * RING_BYTES : OUT_BYTES, LDS_BYTES = SCALES_AT + BM * 4;      // the tokens' scales lie behind
+    static constexpr int TOKEN_PIECES = (BM + 63) / 64;      // loads that bring them, a wave each
+    static constexpr __host__ __device__ bool loads_token(int piece, int lane) { return BM % 64 == 0 || piece * 64 + lane < BM; }      // a last piece may be half a wave
     static_assert(X_BYTES % (WAVES * 1024) == 0 && W_BYTES % (WAVES * 1024) == 0 && BN % 64 == 0, "a K tile is shared out evenly");
     static_assert(S_PIECES % WAVES == 0 || WAVES % S_PIECES == 0, "waves without a piece of their own repeat another's");
     static_assert(LOADS * (STAGES - 1) < 64, "the count of loads in flight has six bits");
@@ -292,9 +294,8 @@ __global__ __launch_bounds__(C::THREADS, 2) void grouped_tile_kernel(const uint8
     // the tokens' scales, first of all loads; waves without a piece of their own repeat another's
     {
         const __amdgpu_buffer_rsrc_t tr = __builtin_amdgcn_make_buffer_rsrc((void *)(token_scale + m0), 0, min(C::BM, M - m0) * 4, RSRC_FLAGS);
-        constexpr int PIECES = (C::BM + 63) / 64;
-        const int piece = wave_all % PIECES;
-        if (C::BM % 64 == 0 || lane < C::BM) __builtin_amdgcn_raw_ptr_buffer_load_lds(tr, LDS_PTR(lds + C::SCALES_AT + piece * 256), 4, (piece * 64 + lane) * 4, 0, 0, 0);
+        const int piece = wave_all % C::TOKEN_PIECES;
+        if (C::loads_token(piece, lane)) __builtin_amdgcn_raw_ptr_buffer_load_lds(tr, LDS_PTR(lds + C::SCALES_AT + piece * 256), 4, (piece * 64 + lane) * 4, 0, 0, 0);
     }
 #pragma unroll
     for (int s = 0; s < C::STAGES - 1; ++s) {
