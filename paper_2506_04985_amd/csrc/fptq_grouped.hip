@@ -4,7 +4,7 @@
 //
 // Nibbles are widened to bytes that hold 16 * value as in the other linears, (p << 4) & 0xF0F0F0F0 and p & 0xF0F0F0F0, and the codes of eight k lie
 // in that order, so they are operands as they are.  Of 128 k or fewer, 16 * sum stays below 2^21 in magnitude, which fp32 holds exactly; the 1/16 goes into the
-// token's scale, exactly as well.  Groups of several K tiles take their scale once a tile.
+// output, exactly as well.  Groups of several K tiles take their scale once a tile.
 #include <utility>
 
 #include "fptq_common.h"
@@ -42,6 +42,18 @@ __device__ inline void by_group(v4i &w)
     w = v4i{d0, d1, d2, d3};
 }
 
+// An output of a sum of 16 * value: the 1/16 goes where it loses nothing, into the token's scale, or into the sum where the scale's lowest bits would fall out of fp32's subnormal range (a sum
+// that loses bits then comes to zero in any case).
+struct OutputScale {
+    float of_sum, of_token;
+    __device__ explicit OutputScale(float s) : of_sum(fabsf(s) < 0x1p-122f ? 0.0625f : 1.0f), of_token(fabsf(s) < 0x1p-122f ? s : s * 0.0625f) {}
+    template <class T>
+    __device__ T operator()(T sum) const
+    {
+        return sum * of_sum * of_token;
+    }
+};
+
 // Few tokens.  A workgroup owns 16 RT channels of 16 tokens, its waves split K (wave w takes K tiles w, w + WAVES, ...) with one K tile in flight each and
 // several workgroups a CU.  Bound: HBM, the weights once, streamed.  Tokens are the rows of the MFMA's result and channels its columns, so that a lane has one channel, and
 // one scale of it a group.  The waves' fp32 sums meet in LDS and are added in order.
@@ -71,7 +83,7 @@ __global__ __launch_bounds__(64 * WAVES) void grouped_few_kernel(const uint8_t *
     // what the thread's output will need, fetched now: the kernel is too short to end on a memory latency
     const int t_out = m0 + tid / (16 * RT), n_out = n0 + tid % (16 * RT);
     const bool stores = tid < RT * 256 && t_out < M && n_out < N;
-    const float ts = stores ? token_scale[t_out] * 0.0625f : 0.0f;
+    const OutputScale scaled(stores ? token_scale[t_out] : 0.0f);
 
     v4f sum[RT];
 #pragma unroll
@@ -124,7 +136,7 @@ __global__ __launch_bounds__(64 * WAVES) void grouped_few_kernel(const uint8_t *
     float v = red[0][tid];
 #pragma unroll
     for (int i = 1; i < WAVES; ++i) v += red[i][tid];
-    v *= ts;
+    v = scaled(v);
     if (y_type == FPTQ_F32)
         static_cast<float *>(y)[(int64_t)t_out * N + n_out] = v;
     else
@@ -139,7 +151,7 @@ typedef v4f v4f_anywhere __attribute__((aligned(4)));
 constexpr int PARTIAL = 2;      // beside FPTQ_BF16 and FPTQ_F32: the sums as they are
 __device__ inline void store_four(v4f v, float scale, int t, int n, int N, void *y, int y_type)
 {
-    v *= scale * 0.0625f;
+    v = OutputScale(scale)(v);
     if (y_type == FPTQ_F32) {
         float *const to = static_cast<float *>(y) + (int64_t)t * N + n;
         if (n + 4 <= N) {

@@ -193,3 +193,24 @@ def test_a_run_of_them_as_a_layer_makes_it():
         assert np.array_equal(fptq.fptq_unpack8(c2, M, F).cpu().numpy(), q) and np.array_equal(t2.cpu().numpy(), t)
         want, mass = grouped.linear(q, t, w2.cpu().numpy(), group, s2.cpu().numpy())
         check(y, want, mass, F, group)
+
+
+@pytest.mark.parametrize("kernel,splits", [(k, 1) for k in range(1, 15)] + [(1, 2), (8, 3)])
+@pytest.mark.parametrize("group", [64, 128])
+def test_subnormal_scales_keep_their_bits(kernel, splits, group, forced):
+    """Token scales of 2^-130 and below with bits down to fp32's last, against sums of 2^16 and more: every output is a number that fp32 holds.  And sums that are tiny behind large scales."""
+    M, N, K = 70, 96, 640
+    rng = np.random.default_rng(kernel)
+    codes, w = np.zeros((M, K), np.int8), np.zeros((N, K), np.int8)
+    codes[:, 3], codes[np.arange(M), 128 + np.arange(M)] = 1, rng.integers(-3, 4, M)
+    w[:, 3], w[:, 128:128 + M] = rng.integers(1, 4, N), 1
+    ws = np.full((-(-K // group), N), 2.0 ** 16, np.float32)
+    s = (2.0 ** -130 * (1 + rng.integers(0, 1 << 19, M) * 2.0 ** -19)).astype(np.float32)
+    s[::7], s[1::7], s[2::7] = 2.0 ** -149, 2.0 ** -122, 2.0 ** -122 * (1 + 2.0 ** -20)
+    y, _ = grouped.linear(codes, s, w, group, ws)
+    assert np.array_equal(y, y.astype(np.float32))
+    forced(kernel, splits)
+    assert np.array_equal(run(codes, s, w, ws, group).cpu().double().numpy(), y)
+    s, ws = np.full(M, 2.0 ** 100, np.float32), np.full_like(ws, 2.0 ** -140)
+    y, _ = grouped.linear(codes, s, w, group, ws)
+    assert np.array_equal(run(codes, s, w, ws, group).cpu().double().numpy(), y)
