@@ -532,6 +532,8 @@ static float few_estimate(const FewCost &c, int64_t M, int64_t N, int64_t kt, in
     return c.start + (float)steps * (c.latency + (float)each * c.each);
 }
 
+static int64_t partial_bytes(int64_t M, int64_t N) { return M * ((N + 3) / 4 * 16); }      // of the sums of a range of K
+
 // What a call takes: 0 .. 9 a tile, 10 + i the few-token kernel FEW_COSTS[..][i], 13 the one of eight waves and 16 channels; into how many ranges K is split between workgroups.
 struct Choice {
     int kernel, splits;
@@ -565,7 +567,7 @@ static Choice grouped_choice(int64_t M, int64_t N, int64_t K, int gt, int64_t sc
     if (M <= 64)
         for (int i = 0; i < 3; ++i) offer(TILES + i, 1, few_estimate(FEW_COSTS[gt >> 1][i], M, N, kt, cus));
     // Few tiles and a long K: its ranges go to workgroups of their own, and a second launch adds their sums.
-    const int64_t range = M * ((N + 3) / 4 * 16);      // bytes of a range's sums
+    const int64_t range = partial_bytes(M, N);
     for (int i = 0; i < TILES; ++i) {
         const int64_t tiles = tiles_of(costs[i], M, N);
         for (int splits = 2; splits <= 8 && tile_serves(i, gt) && tiles * splits <= 2 * cus && kt / splits >= 8 && splits * range <= scratch; ++splits)
@@ -684,7 +686,7 @@ static Choice chosen(int64_t M, int64_t N, int64_t K, int64_t group, int64_t scr
 {
     const int code = g_forced_grouped.load(std::memory_order_relaxed), forced = code % 16, splits = code / 16;
     if (!forced) return grouped_choice(M, N, K, group == 32 ? 4 : group == 64 ? 2 : 1, scratch);
-    const bool room = forced <= TILES && splits <= k_tiles(K) && splits * M * ((N + 3) / 4 * 16) <= scratch;
+    const bool room = forced <= TILES && splits <= k_tiles(K) && splits * partial_bytes(M, N) <= scratch;
     return {forced - 1, room ? splits : 1};
 }
 
@@ -692,7 +694,7 @@ constexpr int64_t MOST_SCRATCH = (int64_t)64 << 20;
 int64_t grouped_scratch_bytes(int64_t M, int64_t N, int64_t K, int64_t group)
 {
     const Choice c = chosen(M, N, K, group, MOST_SCRATCH);
-    return c.splits > 1 ? c.splits * M * ((N + 3) / 4 * 16) : 0;
+    return c.splits > 1 ? c.splits * partial_bytes(M, N) : 0;
 }
 int grouped_kernel(int64_t M, int64_t N, int64_t K, int64_t group) { return chosen(M, N, K, group, 0).kernel; }
 
@@ -700,7 +702,8 @@ hipError_t launch_grouped_linear(const uint8_t *x, const float *token_scale, con
                                  void *y, int y_type, void *scratch, int64_t scratch_bytes, hipStream_t s)
 {
     const int64_t kt = k_tiles(K), per = group > KT ? (group / KT < kt ? group / KT : kt) : 1;
-    const Choice choice = chosen(M, N, K, group, scratch ? (scratch_bytes < MOST_SCRATCH ? scratch_bytes : MOST_SCRATCH) : 0);
+    Choice choice = chosen(M, N, K, group, scratch ? MOST_SCRATCH : 0);
+    if (choice.splits > 1 && choice.splits * partial_bytes(M, N) > scratch_bytes) choice = chosen(M, N, K, group, 0);      // too little counts as none, so that results depend on one thing less
     const GroupedCall c = {x, token_scale, w, (int)M, (int)N, (int)kt, (int)((K - 1) / group + 1), (uint32_t)per, scales, y, y_type, s, choice.splits, (float *)scratch};
     return group == 32 ? launch_choice<4>(choice.kernel, c) : group == 64 ? launch_choice<2>(choice.kernel, c) : launch_choice<1>(choice.kernel, c);
 }

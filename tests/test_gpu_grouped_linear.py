@@ -214,3 +214,28 @@ def test_subnormal_scales_keep_their_bits(kernel, splits, group, forced):
     s, ws = np.full(M, 2.0 ** 100, np.float32), np.full_like(ws, 2.0 ** -140)
     y, _ = grouped.linear(codes, s, w, group, ws)
     assert np.array_equal(run(codes, s, w, ws, group).cpu().double().numpy(), y)
+
+
+@pytest.mark.parametrize("M,N,K,group", [(24, 4096, 14336, 128), (64, 2048, 16384, 64), (100, 1000, 16000, 32), (130, 2048, 28672, 128), (33, 300, 16384, 128)])
+def test_scratch_that_is_too_small_counts_as_none(M, N, K, group):
+    """Bit by bit, however little is missing: no call takes as many ranges as happen to fit."""
+    tiles, g = -(-K // 128), torch.Generator(device="cuda").manual_seed(M)
+    x = torch.randint(-127, 128, (tiles * M * 128,), dtype=torch.int8, device="cuda", generator=g)
+    w = torch.randint(0, 256, (tiles * N * 64,), dtype=torch.uint8, device="cuda", generator=g)
+    s, ws = torch.rand((M,), device="cuda", generator=g), torch.rand((-(-K // group), N), device="cuda", generator=g)
+    need = fptq.fptq_w4a8_linear_scratch_bytes(M, N, K, group)
+    scratch = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    assert need > 0
+
+    def call(bytes, null=False):
+        y = torch.empty((M, N), device="cuda")
+        fptq._check(fptq.lib().fptq_w4a8_linear(fptq._ptr(x), fptq._ptr(s), fptq._ptr(w), M, N, K, group, fptq._ptr(ws), fptq._ptr(y), 1, None if null else fptq._ptr(scratch), bytes,
+                                                fptq._stream()))
+        return y
+    without = call(0, null=True)
+    assert torch.equal(call(need, null=True), without) and torch.equal(call(0), without)
+    for bytes in (need - 1, need - 1 - need // 4, need // 2, need // 3):
+        assert torch.equal(call(bytes), without)
+    assert not bool(scratch.any())
+    call(need)
+    assert bool(scratch.any())
