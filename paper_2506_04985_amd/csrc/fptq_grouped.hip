@@ -487,9 +487,9 @@ constexpr TileCost COSTS[3][TILES] = {      // groups of 128 and more, of 64, of
         {256, 128, 2, 1, 0.00f, {0.00f}, {0.00f}},
         {256, 96, 2, 1, 1.05f, {5.05f}, {2.65f}},
         {256, 64, 2, 1, 0.00f, {0.00f}, {0.00f}},
-        {128, 64, 1, 3, 3.83f, {0.00f, 1.16f, 3.61f}, {0.83f, 1.09f, 1.64f}},
+        {128, 64, 1, 2, 2.53f, {1.32f, 2.59f}, {0.83f, 1.07f}},
         {128, 64, 2, 1, 1.27f, {2.82f}, {1.05f}},
-        {128, 32, 2, 2, 1.91f, {1.90f, 4.50f}, {0.88f, 1.73f}},
+        {128, 32, 2, 1, 1.67f, {2.24f}, {0.87f}},
         {64, 64, 4, 1, 1.40f, {2.92f}, {1.40f}},
         {64, 32, 8, 1, 1.56f, {1.99f}, {1.24f}},
     },
@@ -505,8 +505,27 @@ template <int GT> using Tile6 = Tile<4, 1, 1, 2, 3, 2, GT>;
 template <int GT> using Tile7 = Tile<2, 1, 2, 1, 3, 2, GT>;
 template <int GT> using Tile8 = Tile<1, 1, 2, 2, 3, 4, GT>;
 template <int GT> using Tile9 = Tile<1, 1, 2, 1, 2, 8, GT>;
-// groups of 32: the first would spill, the third has no room for its scales in LDS
+// groups of 32: 256 x 256 and 256 x 128 would spill (3 and 7 registers), 256 x 64 has no room for its scales in LDS (172288 bytes)
 constexpr bool tile_serves(int i, int gt) { return gt < 4 || (i != 0 && i != 2 && i != 4); }
+
+// Workgroups of a tile kernel that a CU's LDS holds, given out in pieces of 1280 bytes; the table may not count on more.
+template <class C>
+constexpr int lds_room()
+{
+    return 160 * 1024 / ((C::LDS_BYTES + 1279) / 1280 * 1280);
+}
+template <int GT>
+constexpr bool fit_in_lds()
+{
+    const TileCost(&costs)[TILES] = COSTS[GT >> 1];
+    bool fit = costs[1].fit <= lds_room<Tile1<GT>>() && costs[3].fit <= lds_room<Tile3<GT>>() && costs[5].fit <= lds_room<Tile5<GT>>() && costs[6].fit <= lds_room<Tile6<GT>>() &&
+               costs[7].fit <= lds_room<Tile7<GT>>() && costs[8].fit <= lds_room<Tile8<GT>>() && costs[9].fit <= lds_room<Tile9<GT>>();
+    if constexpr (tile_serves(0, GT)) fit = fit && costs[0].fit <= lds_room<Tile0<GT>>();
+    if constexpr (tile_serves(2, GT)) fit = fit && costs[2].fit <= lds_room<Tile2<GT>>();
+    if constexpr (tile_serves(4, GT)) fit = fit && costs[4].fit <= lds_room<Tile4<GT>>();
+    return fit;
+}
+static_assert(fit_in_lds<1>() && fit_in_lds<2>() && fit_in_lds<4>(), "more workgroups than LDS holds");
 
 static int64_t tiles_of(const TileCost &c, int64_t M, int64_t N) { return ((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn); }
 

@@ -1,10 +1,10 @@
 """What the tile kernels of the 8-bit linear may touch and hold, from their constants: a host-only compilation of the source, no GPU needed."""
 import os
+import re
 import subprocess
 
-import pytest
-
 from paper_2506_04985_amd import build
+from test_code_objects import code_objects, kernels  # noqa: F401
 
 HEAD = r"""
 #include "fptq_grouped.hip"
@@ -55,3 +55,28 @@ template <class C> struct Within {
 };
 static_assert(all<Within>(Tiles()), "a token's scale is missing or lies outside");
 """)
+
+
+def test_the_table_of_times_counts_on_as_many_workgroups_as_a_cu_holds(kernels):  # noqa: F811
+    """160 KB of LDS in pieces of 1280 bytes, and 512 registers a lane of a SIMD in pieces of 8, shared by at most eight waves."""
+    text = open(os.path.join(build.CSRC, "fptq_grouped.hip")).read()
+    shapes = [tuple(int(v) for v in re.findall(r"\d+", m)) for m in re.findall(r"using Tile\d = Tile<([^G]*), GT>;", text)]
+    table = re.search(r"COSTS\[3\]\[TILES\] = \{(.*?)\n\};", text, re.S).group(1)
+    rows = [(int(a), int(b), int(c), int(d)) for a, b, c, d in re.findall(r"\{(\d+), (\d+), (\d+), (\d+), \d", table)]
+    assert len(shapes) == 10 and len(rows) == 30
+    registers = {}
+    for name, notes in kernels.items():
+        m = re.search(r"grouped_tile_kernelINS_4TileI((?:Li\d+E)+)E", name)
+        if m:
+            registers[tuple(int(v) for v in re.findall(r"\d+", m.group(1)))] = int(re.search(r"\.vgpr_count:\s+(\d+)", notes).group(1))
+    assert len(registers) == 27
+    for kind, groups in enumerate((1, 2, 4)):
+        for shape, (bn, bm, sets, fit) in zip(shapes, rows[10 * kind:]):
+            waves_n, waves_m, tn, tm, stages, ks = shape
+            assert (bn, bm, sets) == (32 * waves_n * tn, 32 * waves_m * tm, ks)
+            if shape + (groups,) not in registers:
+                continue
+            ring, out = ks * stages * (bm * 128 + bn * 64 + bn * groups * 4), ks * waves_m * 32 * bn * 4
+            lds = max(ring, out) + bm * 4
+            waves = min(8, 512 // (-(-registers[shape + (groups,)] // 8) * 8)) * 4 // (waves_n * waves_m * ks)
+            assert fit == min(160 * 1024 // (-(-lds // 1280) * 1280), waves), (groups, bn, bm, sets)
