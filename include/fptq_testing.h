@@ -44,7 +44,7 @@ int fptq_linear_launch_plan(int64_t M, int64_t N, int64_t K, int with_workspace,
 
 /* The kernel that fptq_w4a8_linear takes: 0 chooses it per problem (default); 1 .. 10 force a tile, in `splits` ranges of K (1 .. 8) where the call has scratch for them, 11 .. 14 a few-token
  * kernel, for tests and sweeps; fptq_w4a8_linear_scratch_bytes follows.  A tile that does not serve the call's groups (1, 3 and 5: groups of 32) makes it fail with FPTQ_ERR_HIP.
- * fptq_grouped_kernel returns the number that a call without scratch would take, host only. */
+ * fptq_grouped_kernel returns the number that a call without scratch would take, or the error with which the call would refuse these sizes, host only. */
 int fptq_set_grouped_kernel(int kernel, int splits);
 int fptq_grouped_kernel(int64_t M, int64_t N, int64_t K, int64_t group);
 

@@ -818,6 +818,10 @@ int fptq_set_grouped_kernel(int kernel, int splits)
     return FPTQ_OK;
 }
 
-int fptq_grouped_kernel(int64_t M, int64_t N, int64_t K, int64_t group) { return M < 1 || N < 1 || K < 1 || group < 1 ? FPTQ_ERR_SHAPE : 1 + grouped_kernel(M, N, K, group); }
+int fptq_grouped_kernel(int64_t M, int64_t N, int64_t K, int64_t group)
+{
+    const int rc = check_grouped("fptq_grouped_kernel", M, N, K, group);
+    return rc ? rc : 1 + grouped_kernel(M, N, K, group);
+}
 
 }  // extern "C"

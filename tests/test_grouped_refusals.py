@@ -76,3 +76,11 @@ def test_kernel_choice_is_host_arithmetic():
         for N in (64, 1000, 5000, 40000):
             for K in (128, 1000, 8000):
                 assert of(M, N, K, 32) not in (1, 3, 5) and 1 <= of(M, N, K, 128) <= (13 if M <= 64 else 10)
+
+
+@pytest.mark.parametrize("M,N,K,group", [(4, 5, 300, 33), (4, 5, 300, 96), (4, 5, 300, 130), ((1 << 24) + 1, 5, 300, 64), (4, 1 << 25, 300, 64), (4, 5, 1 << 25, 64), (1 << 24, (1 << 12) + 1, 300, 64),
+                                         (1 << 40, 1, 300, 64)])
+def test_no_kernel_is_named_for_a_call_that_is_refused(M, N, K, group):
+    L = fptq.lib()
+    assert L.fptq_w4a8_linear(*[dict(LINEAR, M=M, N=N, K=K, group=group)[k] for k in LINEAR]) == SHAPE
+    assert L.fptq_grouped_kernel(M, N, K, group) == SHAPE and b"fptq_grouped_kernel" in L.fptq_last_error()
