@@ -86,7 +86,7 @@ bool truth(PyObject *o)
 }
 
 // Whether torch's empty() would do nothing but allocate: no dispatch mode, transform or profiler wants to see it, and nothing is to be filled.  Outputs on the current device then come straight
-// from the allocator that it takes, 0.3 us an output less (norm, residual and scale: 6.2 -> 5.3 us a call).
+// from the allocator that it takes, 0.3 us an output less, of which this look takes 0.02 to 0.05 (norm, residual and scale: 6.2 -> 5.4 us a call).
 bool plain_allocation()
 {
     const at::Context &context = at::globalContext();

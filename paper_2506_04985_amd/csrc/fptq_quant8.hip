@@ -7,7 +7,7 @@
 // The norm's factor is the same for a whole row, so it goes into the token's scale and not into the codes: one pass with one exchange between
 // the waves of a row (a sum and a maximum at once), and a row's codes do not wait for a division and a root in 64 bits.  The row stays in registers
 // from its load to its codes.  Bound: HBM, 2 to 4 bytes read and 1 to 3 written per value: norm with residual and gain 8192 x 8192 83 us, 5.65 TB/s (a copy of 2 GiB reaches 4.92), VALU busy in
-// 40 % of the cycles; gated 4096 x 14336 58 us, 5.06 TB/s.  Few rows are a chain of latencies: launch, row, exchange, store (norm 1 x 4096 2.2 us in a kernel trace, gated 16 x 14336 5.4 to 5.8).
+// 40 % of the cycles; gated 4096 x 14336 58 us, 5.06 TB/s.  Few rows are a chain of latencies: launch, row, exchange, store (norm 1 x 4096 2.2 us in a kernel trace, gated 16 x 14336 6.3 to 6.7).
 #include "fptq_common.h"
 
 namespace fptq {
@@ -44,7 +44,8 @@ __device__ inline float silu(float g)
 }
 
 // silu of the bf16 values of magnitude 2^-14 to 2^7, sign by sign in the order of their patterns: 21 KB of LDS, read once a workgroup, in place of 33 instructions a value, most of them in
-// 64 bits, which bound the kernel (4096 x 14336 83 us).  Made by the compiler with the same series, in 64 bits and rounded once.
+// 64 bits, which bound the kernel (4096 x 14336 83 us).  That is for gates like those of a layer, of deviation 1.5; smaller ones fall below the table and are computed, a wave's chunk at a time: 4096 x 14336 56 us with
+// deviation 1.5, 63 with 0.1, 84 with 0.02, 92 with zeros.  Made by the compiler with the same series, in 64 bits and rounded once.
 constexpr int SILU_FIRST = (127 - 14) << 7, SILU_COUNT = 21 << 7;
 struct SiluTable {
     float value[2 * SILU_COUNT];
@@ -112,7 +113,7 @@ __device__ inline void gated_eight(const uint32_t (&aw)[4], const uint32_t (&bw)
     for (int j = 0; j < 4; ++j) z[2 * j] = table[at[j] & 0xffffu], z[2 * j + 1] = table[at[j] >> 16];
     if (__any(live && max(far.x, far.y) >= SILU_COUNT)) {
 #pragma unroll 1
-        for (int j = 0; j < 4; ++j) {      // rolled: gates of zero and beyond the table are few
+        for (int j = 0; j < 4; ++j) {      // rolled: gates of zero and beyond the table are taken to be few
             const float s0 = silu(low_f32(aw[j])), s1 = silu(high_f32(aw[j]));
             if (j == 0) z[0] = s0, z[1] = s1;
             if (j == 1) z[2] = s0, z[3] = s1;
