@@ -352,13 +352,14 @@ hipError_t launch_unpack8(const uint8_t *packed, int64_t rows, int64_t K, int8_t
 
 constexpr int64_t MOST_WORKGROUPS = (int64_t)1 << 20;      // of a launch, whose threads have to stay below 2^32
 
-// Workgroups of the gated kernel with the table that a CU runs at once: the table's LDS (7), the CU's 32 waves, or from two chunks a lane on the registers.
+// Workgroups of the gated kernel with the table that a CU runs at once, by the table's LDS (7), a SIMD's eight waves (seven for ragged rows, whose kernels take more than 100 scalar registers), or
+// from three chunks a lane on the vector registers.
 template <int WPR, int CH, bool RAGGED>
 constexpr int resident()
 {
     if (WPR <= 4) return CH <= 2 ? 7 : 5;
-    if (WPR == 8) return CH <= 2 ? 4 : CH == 3 && !RAGGED ? 3 : 2;
-    return CH == 1 || (CH == 2 && !RAGGED) ? 2 : 1;
+    if (WPR == 8) return CH == 4 ? 2 : (CH == 3 ? 3 : 4) - RAGGED;
+    return CH <= 2 && !RAGGED ? 2 : 1;
 }
 
 template <int KIND, int WPR, int CH, bool TABLE>
@@ -386,7 +387,8 @@ static hipError_t launch(const uint16_t *a, const uint16_t *b, const uint16_t *g
     auto aligned = [](const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
     const bool vec = K % 8 == 0 && aligned(a) && aligned(b) && aligned(gain) && aligned(sum_out) && a_stride % 8 == 0 && b_stride % 8 == 0;
     // As many threads as the row has chunks, two or three chunks each where that is more than 512, on 17078 sizes measured with data in no cache (rows / workgroup): the rule is within 1 % of the
-    // best of 22 shapes on average, 3 to 7 % at the 95th percentile.  us, norm with residual, rows of 7391 values / 8192 / 14336: 333 x 16 waves of one chunk 9.5, 8 of two 7.6; 8192 x 97.6 and 92.2;
+    // best of 22 shapes on average, 3 to 7 % at the 95th percentile (gated rows on 30593 sizes: beyond 4096 values 0 to 3 % on average, in shorter ones up to 5 % with 2048 rows, 0 to 22 % with more, where a
+    // wave or two a row with three or four chunks a lane would do better).  us, norm with residual, rows of 7391 values / 8192 / 14336: 333 x 16 waves of one chunk 9.5, 8 of two 7.6; 8192 x 97.6 and 92.2;
     // 4096 x 16 of two 91.3, 8 of four 95.0.  The gated kernel reads its table where there are enough values to a workgroup: 4096 x 14336 83.6 without, 55.6 with it, 32 x 4096 3.4 and 4.2.
 #define FPTQ_ROWS(WPR, CH, TABLE) return launch_rows<KIND, WPR, CH, TABLE && KIND == GATED>(vec, a, b, gain, M, K, a_stride, b_stride, rms, eps, out, scale, sum_out, s)
     if (M <= 0x7fffffff && K <= 32768) {
