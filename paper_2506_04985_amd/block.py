@@ -116,6 +116,7 @@ def main(prompt=4096, steps=64, sequences=4, heads=32, kv_heads=8, head_dim=128,
     y, us = timed(lambda: layer.prompt(x, cache, table, lengths, cu), 10)
     print(f"prompts of {sequences} x {prompt // sequences} tokens: {us:.1f} us, output {tuple(y.shape)}, finite: {bool(torch.isfinite(y).all())}")
     if mlp_width:
+        mlp(y, x)
         (y, _), us = timed(lambda: mlp(y, x), 10)
         print(f"their MLP half: {us:.1f} us, output {tuple(y.shape)}, finite: {bool(torch.isfinite(y).all())}")
     # the token loop as a server runs it: one captured step, replayed on growing lengths

@@ -83,3 +83,17 @@ def test_the_command_runs_it(capsys):
     block.main(prompt=256, steps=3, sequences=2, heads=4, kv_heads=2, head_dim=64, width=256, mlp_width=500, group=64)
     lines = capsys.readouterr().out.strip().splitlines()
     assert len(lines) == 4 and all("finite: True" in l for l in lines)
+
+
+def test_the_command_times_no_first_call(monkeypatch, capsys):
+    """What it prints holds no call that allocates: each half runs once before its prompts are timed."""
+    events, record = [], torch.cuda.Event.record
+    monkeypatch.setattr(torch.cuda.Event, "record", lambda self, *a: (events.append("time"), record(self, *a))[1])
+    for kind, name in ((block.Attention, "prompt"), (block.Mlp, "__call__")):
+        def spy(self, *a, call=getattr(kind, name), kind=kind):
+            events.append(kind.__name__)
+            return call(self, *a)
+        monkeypatch.setattr(kind, name, spy)
+    block.main(prompt=256, steps=3, sequences=2, heads=4, kv_heads=2, head_dim=64, width=256, mlp_width=500, group=64)
+    half = lambda name: [name, "time"] + 10 * [name] + ["time"]
+    assert events[:26] == half("Attention") + half("Mlp")
