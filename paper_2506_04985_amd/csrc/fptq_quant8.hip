@@ -368,7 +368,7 @@ static hipError_t launch_rows(bool vec, const uint16_t *a, const uint16_t *b, co
 {
     int64_t blocks = WPR == 1 ? (M + 3) / 4 : M;
     if (TABLE) {      // a workgroup reads the table once and goes on from row to row: as many as fit the device together, and where a CU holds one, as many as come to the same number of rows each
-        // (on 1100 sizes: so 4 % faster than with the same number of rows each where a CU holds several, 1 % slower where it holds one; 600 x 28001 34.1 us with two workgroups a CU asked for, 26.2 with the one it holds)
+        // (on 1100 sizes: so 4 % faster than with the same number of rows each where a CU holds several, 1 % slower where it holds one; 600 x 28001 34.0 us with two workgroups a CU asked for, 26.5 with the one it holds)
         const int64_t cus = device_cus_or_default(), a_cu = vec ? resident<WPR, CH, false>() : resident<WPR, CH, true>(), room = cus * a_cu, each = (blocks + room - 1) / room;
         blocks = a_cu == 1 ? (blocks + each - 1) / each : blocks < room ? blocks : room;
     }
